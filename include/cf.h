@@ -511,6 +511,120 @@ cf_status cf_goodput_curve(const cf_fine_out *fine, int32_t n_plans, int32_t K, 
  * lowest index, written to best_dev[0]. */
 cf_status cf_select_best(const double *goodput_dev, int32_t n, int32_t *best_dev, void *stream);
 
+/* ------------------------------------------------------------------ attention over a paged cache
+ * The attention of an LLM executor's iteration (prefill and decode steps,
+ * Sec. 2) and the page bookkeeping it reads: what a profile of an executor
+ * (Sec. 5.1) measures where an iteration's time depends on request lengths.
+ *
+ * Cache: keys and values of one layer, each [n_pages][n_kv_heads][page]
+ * [head_dim] of 16-bit elements; page is a power of two, 16..256.  Slot s is
+ * token s % page of page s / page.  A request's tokens are at table[request]
+ * [position / page], position % page.  head_dim is a multiple of 8, 8..256;
+ * pointers to elements are 16-byte aligned and strides (in elements) are
+ * multiples of 8.  Lengths, page ids and starts live in device memory and are
+ * not trusted: every read and write stays inside the stated arrays whatever
+ * they hold. */
+#define CF_BF16 0
+#define CF_F16 1
+
+/* cf_kv_map per-request status */
+#define CF_KV_TOO_LONG 1 /* negative length, or past the table row or the token arrays */
+#define CF_KV_NO_PAGE 2  /* the free list ends before the request's pages */
+
+typedef struct cf_kv_cache {
+  void *k_dev, *v_dev; /* [n_pages][n_kv_heads][page][head_dim] */
+  int32_t n_pages, page, n_kv_heads, head_dim;
+  int32_t dtype; /* CF_BF16 / CF_F16, also of queries, keys, values and outputs */
+} cf_kv_cache;
+
+/* Block tables and slot maps of one step from request lengths (the batches an
+ * LLM executor forms, Sec. 2).  Request i has ctx_len_dev[i] cached tokens and
+ * new_len_dev[i] new ones, packed in request order; its new pages are the next
+ * ceil((ctx+new)/page) - ceil(ctx/page) entries of free_dev [n_free] from
+ * *head_dev on, in request order, entered in its row of table_dev
+ * [n_seq][max_pages] (updated in place; other entries are left).
+ * Outputs: q_start_dev[n_seq + 1] running sums of the new lengths;
+ * kv_len_dev[i] = ctx + new; per packed token (n_tok of them) slot_dev and
+ * pos_dev, its position (at most 2^31 - 1); *head_out_dev (another word than *head_dev) the first
+ * free entry left.  A refused request (status_dev[i] != 0) takes no page: kv_len 0,
+ * slots -1, its tokens still counted by q_start.  CF_KV_NO_PAGE holds for
+ * every request that needs pages from the first that finds too few.  Tokens
+ * past q_start_dev[n_seq] get slot -1 and position 0; lengths below 0 count
+ * as 0.  Asynchronous; may be captured in a graph.
+ * Errors: CF_EINVAL (sizes, page, NULL arrays). */
+cf_status cf_kv_map(int32_t n_seq, const int32_t *ctx_len_dev, const int32_t *new_len_dev, int32_t page,
+                    int32_t *table_dev, int32_t max_pages, const int32_t *free_dev, int32_t n_free,
+                    const int32_t *head_dev, int32_t n_tok, int32_t *q_start_dev, int32_t *kv_len_dev,
+                    int64_t *slot_dev, int32_t *pos_dev, int32_t *head_out_dev, int32_t *status_dev, void *stream);
+
+/* Keys and values of n_tok new tokens into the cache: element [t][h][d] of
+ * k_dev (token and head strides k_tok, k_head; v likewise) goes to slot_dev[t].
+ * Slots outside the cache (-1 among them) are skipped; of two tokens with one
+ * slot, either is kept.
+ * Errors: CF_EINVAL (sizes, alignment, NULL arrays). */
+cf_status cf_kv_write(const cf_kv_cache *cache, int32_t n_tok, const void *k_dev, int64_t k_tok, int64_t k_head,
+                      const void *v_dev, int64_t v_tok, int64_t v_head, const int64_t *slot_dev, void *stream);
+
+/* One step's attention: n_tok new tokens of n_seq requests (starts
+ * q_start_dev, cached lengths with the new tokens kv_len_dev, as cf_kv_map
+ * writes them), n_heads query heads, query head h reading key/value head
+ * h / (n_heads / n_kv_heads).  max_new bounds a request's new tokens as far
+ * as the caller knows (n_tok if it does not); it picks kernels, not results.
+ * work_dev: cf_attn_plan_bytes(...) bytes, 16-byte aligned, the caller's; it
+ * holds the plan and the partial results of split contexts, so calls that
+ * share it must not overlap. */
+typedef struct cf_attn_desc {
+  int32_t n_seq, n_tok, max_new;
+  int32_t n_heads, n_kv_heads, head_dim;
+  const int32_t *q_start_dev; /* [n_seq + 1] */
+  const int32_t *kv_len_dev;  /* [n_seq] */
+  void *work_dev;
+  uint64_t work_bytes;
+} cf_attn_desc;
+
+/* Bytes of work_dev (host only; the device pointers are not read).
+ * Errors: CF_EINVAL (sizes). */
+cf_status cf_attn_plan_bytes(const cf_attn_desc *d, uint64_t *bytes);
+
+/* The step's plan, made on the device from the lengths and written to
+ * work_dev: which (request, rows, keys) each workgroup takes, long contexts
+ * split so that few requests fill the GPU.  One call serves every layer's
+ * cf_attn_paged of the step.
+ * Errors: CF_EINVAL (sizes, NULL arrays, work_bytes too small). */
+cf_status cf_attn_plan(const cf_attn_desc *d, void *stream);
+
+/* Attention of the new tokens over the cache, the new tokens' own keys and
+ * values included (written before).  Row (t, h), the j-th new token of request
+ * i, sees keys 0 .. kv_len - new + j: out = sum_k p_k v_k / sum_k p_k,
+ * p_k = exp(scale q.k).  A row that sees no key (kv_len 0, or fewer keys than
+ * new tokens) gives 0, and lse -inf.  Keys past kv_len are never used, whatever
+ * they hold; pages outside the cache read as zeros.  q_dev [n_tok][n_heads]
+ * [head_dim] with strides q_tok and q_head; out_dev packed; lse_dev
+ * [n_tok][n_heads] float, log of the sum of the p_k, or NULL.  Sums, the
+ * softmax's maximum and sum, and outputs are kept in 32 bits; the p_k are
+ * rounded to the element type for their product with the values.
+ * Errors: CF_EINVAL (sizes, alignment, scale not finite and > 0, NULL arrays). */
+cf_status cf_attn_paged(const cf_attn_desc *d, const cf_kv_cache *cache, const int32_t *table_dev,
+                        int32_t max_pages, const void *q_dev, int64_t q_tok, int64_t q_head, float scale,
+                        void *out_dev, float *lse_dev, void *stream);
+
+/* Attention of whole packed sequences, keys and values not in a cache: an
+ * encoder's batch, or prompts without cached tokens.  Sequence i has queries
+ * q_start_dev[i] .. q_start_dev[i+1]-1 of q_dev [n_q][n_heads][head_dim] and
+ * keys k_start_dev[i] .. of k_dev, v_dev [n_k][n_kv_heads][head_dim].  With
+ * causal != 0 the j-th of nq queries sees keys 0 .. nk - nq + j (the last
+ * query sees all), else all.  Rows that see none, lse and rounding as in
+ * cf_attn_paged.  dtype: CF_BF16 / CF_F16.
+ * Errors: CF_EINVAL (sizes, alignment, scale, NULL arrays). */
+typedef struct cf_attn_seqs {
+  int32_t n_seq, n_q, n_k;
+  int32_t n_heads, n_kv_heads, head_dim, dtype, causal;
+  const int32_t *q_start_dev, *k_start_dev; /* [n_seq + 1] */
+  const void *q_dev, *k_dev, *v_dev;
+  int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head; /* strides in elements */
+} cf_attn_seqs;
+cf_status cf_attn_prompt(const cf_attn_seqs *a, float scale, void *out_dev, float *lse_dev, void *stream);
+
 /* Diagnostics for tests: the device primitives applied element-wise.
  * op 0: cf_log(x)  1: cf_exp(x)  2: sqrt(x)  3: x / y  4: uniform(bits of x)
  * y_dev is only read by op 3; out_dev[n]. */

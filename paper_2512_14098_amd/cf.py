@@ -83,6 +83,24 @@ class cf_fine_out(C.Structure):
                 ("lim_instants", C.c_uint64)]
 
 
+class cf_kv_cache(C.Structure):
+    _fields_ = [("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("n_pages", C.c_int32), ("page", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class cf_attn_desc(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("n_tok", C.c_int32), ("max_new", C.c_int32), ("n_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("q_start_dev", C.c_void_p),
+                ("kv_len_dev", C.c_void_p), ("work_dev", C.c_void_p), ("work_bytes", C.c_uint64)]
+
+
+class cf_attn_seqs(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("n_seq", "n_q", "n_k", "n_heads", "n_kv_heads", "head_dim", "dtype",
+                                         "causal")] + [
+        (f, C.c_void_p) for f in ("q_start_dev", "k_start_dev", "q_dev", "k_dev", "v_dev")] + [
+        (f, C.c_int64) for f in ("q_tok", "q_head", "k_tok", "k_head", "v_tok", "v_head")]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise CfError("libcf.so is not built (%s); run __graft_entry__.build()" % LIB_PATH)
@@ -110,6 +128,12 @@ def _load():
         "cf_enum_count": ([vp, vp, vp, i32, vp, vp, vp], i32),
         "cf_enum_plans": ([vp, vp, vp, i32, vp, C.c_uint64, C.c_uint64, i32, vp, vp], i32),
         "cf_select_best": ([vp, i32, vp, vp], i32),
+        "cf_kv_map": ([i32, vp, vp, i32, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp], i32),
+        "cf_kv_write": ([vp, i32, vp, i64, i64, vp, i64, i64, vp, vp], i32),
+        "cf_attn_plan_bytes": ([vp, vp], i32),
+        "cf_attn_plan": ([vp, vp], i32),
+        "cf_attn_paged": ([vp, vp, vp, i32, vp, i64, i64, C.c_float, vp, vp, vp], i32),
+        "cf_attn_prompt": ([vp, C.c_float, vp, vp, vp], i32),
         "cf_math_eval": ([i32, vp, vp, vp, i64, vp], i32),
         "cf_philox_eval": ([vp, vp, vp, i64, vp], i32),
         "cf_release_scratch": ([], i32),
@@ -126,7 +150,8 @@ EXPORTED = ("cf_last_error", "cf_status_str", "cf_version", "cf_trace_gen", "cf_
             "cf_select_topk", "cf_topk_merge", "cf_rate_grid", "cf_eval_fine", "cf_eval_fine_noalloc", "cf_eval_bisect", "cf_eval_mc",
             "cf_eval_mc_curve", "cf_goodput_curve", "cf_pareto",
             "cf_enum_logical", "cf_enum_count", "cf_enum_plans", "cf_enum_screen",
-            "cf_goodput_reduce", "cf_select_best", "cf_math_eval", "cf_philox_eval", "cf_release_scratch")
+            "cf_goodput_reduce", "cf_select_best", "cf_kv_map", "cf_kv_write", "cf_attn_plan_bytes",
+            "cf_attn_plan", "cf_attn_paged", "cf_attn_prompt", "cf_math_eval", "cf_philox_eval", "cf_release_scratch")
 
 
 def lib():
@@ -622,6 +647,152 @@ def cf_select_best(goodput):
     _check(_lib.cf_select_best(_in(goodput, torch.float64, "goodput"), int(goodput.numel()), _p(best), _stream()),
            "cf_select_best")
     return best
+
+
+# ------------------------------------------------------------------ attention over a paged cache
+KV_TOO_LONG, KV_NO_PAGE = 1, 2  # cf_kv_map status
+ATTN_DTYPE = {torch.bfloat16: 0, torch.float16: 1}
+
+
+def _rows(t, what, heads=None, dim=None, dtype=None):
+    """A [tokens][heads][dim] tensor of 16-bit elements as the C ABI reads it: innermost
+    dimension packed, strides multiples of 8 elements, 16-byte aligned (copied where not)."""
+    if t.dim() != 3 or not t.is_cuda:
+        raise CfError("%s: expected a device tensor [tokens][heads][dim]" % what)
+    if t.dtype not in ATTN_DTYPE or (dtype is not None and t.dtype != dtype):
+        raise CfError("%s: expected %s, got %s" % (what, dtype or "bfloat16 or float16", t.dtype))
+    if (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
+        raise CfError("%s: expected [tokens][%s][%s], got %s" % (what, heads, dim, tuple(t.shape)))
+    if t.numel() and (t.stride(2) != 1 or t.stride(0) % 8 or t.stride(1) % 8 or t.data_ptr() % 16):
+        t = torch.empty(tuple(t.shape), dtype=t.dtype, device=t.device).copy_(t)
+    return t
+
+
+def _kv_cache(k_cache, v_cache):
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype:
+        raise CfError("cache: expected two tensors [pages][heads][page][dim] of one shape and type")
+    if k_cache.dtype not in ATTN_DTYPE:
+        raise CfError("cache: expected bfloat16 or float16, got %s" % k_cache.dtype)
+    c = cf_kv_cache()
+    c.k_dev, c.v_dev = _p(k_cache), _p(v_cache)
+    c.n_pages, c.n_kv_heads, c.page, c.head_dim = (int(x) for x in k_cache.shape)
+    c.dtype = ATTN_DTYPE[k_cache.dtype]
+    return c
+
+
+def cf_kv_map(ctx_len, new_len, table, page, free_pages, head, n_tok):
+    """Block tables and slot maps of one step: fills the new pages into ``table`` [n][max_pages]
+    (in place) from ``free_pages``, beginning at ``head`` [1]; n_tok packed new tokens.
+    Returns (q_start [n+1], kv_len [n], slots [n_tok] int64, pos [n_tok], head [1], status [n])."""
+    n, dev = int(ctx_len.numel()), ctx_len.device
+    if table.dim() != 2 or table.shape[0] != n or table.dtype != torch.int32:
+        raise CfError("table: expected int32 [%d][max_pages]" % n)
+    q_start = torch.empty(n + 1, dtype=torch.int32, device=dev)
+    kv_len = torch.empty(n, dtype=torch.int32, device=dev)
+    slots = torch.empty(int(n_tok), dtype=torch.int64, device=dev)
+    pos = torch.empty(int(n_tok), dtype=torch.int32, device=dev)
+    head_out = torch.empty(1, dtype=torch.int32, device=dev)
+    status = torch.empty(n, dtype=torch.int32, device=dev)
+    _check(_lib.cf_kv_map(n, _in(ctx_len, torch.int32, "ctx_len"), _in(new_len, torch.int32, "new_len", n), int(page),
+                          _p(table), int(table.shape[1]), _in(free_pages, torch.int32, "free_pages"),
+                          int(free_pages.numel()), _in(head, torch.int32, "head", 1), int(n_tok), _p(q_start),
+                          _p(kv_len), _p(slots), _p(pos), _p(head_out), _p(status), _stream()), "cf_kv_map")
+    return q_start, kv_len, slots, pos, head_out, status
+
+
+def cf_kv_write(k, v, k_cache, v_cache, slots):
+    """Keys and values [tokens][heads][dim] of new tokens into their slots of the caches
+    [pages][heads][page][dim], in place."""
+    c = _kv_cache(k_cache, v_cache)
+    k = _rows(k, "k", c.n_kv_heads, c.head_dim, k_cache.dtype)
+    v = _rows(v, "v", c.n_kv_heads, c.head_dim, k_cache.dtype)
+    n = int(k.shape[0])
+    if v.shape[0] != n:
+        raise CfError("k and v: %d and %d tokens" % (n, v.shape[0]))
+    _check(_lib.cf_kv_write(C.byref(c), n, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                            v.stride(1), _in(slots, torch.int64, "slots", n), _stream()), "cf_kv_write")
+
+
+class AttnPlan:
+    """A step's attention plan (cf_attn_plan) with the lengths it was made from."""
+
+    def __init__(self, desc, q_start, kv_len, work):
+        self.c, self.q_start, self.kv_len, self.work = desc, q_start, kv_len, work
+
+
+def cf_attn_plan(q_start, kv_len, n_tok, max_new, n_heads, n_kv_heads, head_dim):
+    """The plan of one step's attention, shared by the cf_attn_paged calls of all its layers.
+    max_new: the most new tokens of a request, or n_tok if not known on the host."""
+    n = int(kv_len.numel())
+    d = cf_attn_desc()
+    d.n_seq, d.n_tok, d.max_new = n, int(n_tok), int(max_new)
+    d.n_heads, d.n_kv_heads, d.head_dim = int(n_heads), int(n_kv_heads), int(head_dim)
+    q_start, kv_len = q_start.contiguous(), kv_len.contiguous()
+    d.q_start_dev, d.kv_len_dev = _in(q_start, torch.int32, "q_start", n + 1), _in(kv_len, torch.int32, "kv_len")
+    need = C.c_uint64(0)
+    _check(_lib.cf_attn_plan_bytes(C.byref(d), C.byref(need)), "cf_attn_plan_bytes")
+    work = torch.empty(need.value, dtype=torch.uint8, device=kv_len.device)
+    d.work_dev, d.work_bytes = work.data_ptr(), need.value
+    _check(_lib.cf_attn_plan(C.byref(d), _stream()), "cf_attn_plan")
+    return AttnPlan(d, q_start, kv_len, work)
+
+
+def cf_attn_plan_bytes(n_seq, n_tok, max_new, n_heads, n_kv_heads, head_dim):
+    """Device bytes of such a plan."""
+    d = cf_attn_desc()
+    d.n_seq, d.n_tok, d.max_new = int(n_seq), int(n_tok), int(max_new)
+    d.n_heads, d.n_kv_heads, d.head_dim = int(n_heads), int(n_kv_heads), int(head_dim)
+    need = C.c_uint64(0)
+    _check(_lib.cf_attn_plan_bytes(C.byref(d), C.byref(need)), "cf_attn_plan_bytes")
+    return need.value
+
+
+def cf_attn_paged(plan, q, k_cache, v_cache, table, scale=None, lse=False):
+    """Attention of the step's new tokens q [n_tok][n_heads][dim] over the cache, causal within
+    a request: [n_tok][n_heads][dim], with lse also the rows' log-sum-exp [n_tok][n_heads].
+    scale: head_dim ** -0.5 unless given."""
+    d = plan.c
+    c = _kv_cache(k_cache, v_cache)
+    q = _rows(q, "q", d.n_heads, d.head_dim, k_cache.dtype)
+    if q.shape[0] != d.n_tok:
+        raise CfError("q: expected %d tokens, got %d" % (d.n_tok, q.shape[0]))
+    if table.dim() != 2 or table.shape[0] != d.n_seq:
+        raise CfError("table: expected [%d][max_pages]" % d.n_seq)
+    table = table.contiguous()
+    out = torch.empty(tuple(q.shape), dtype=q.dtype, device=q.device)
+    ls = torch.empty((d.n_tok, d.n_heads), dtype=torch.float32, device=q.device) if lse else None
+    _check(_lib.cf_attn_paged(C.byref(d), C.byref(c), _in(table, torch.int32, "table"), int(table.shape[1]),
+                              q.data_ptr(), q.stride(0), q.stride(1),
+                              float(d.head_dim ** -0.5 if scale is None else scale), _p(out), _p(ls), _stream()),
+           "cf_attn_paged")
+    return (out, ls) if lse else out
+
+
+def cf_attn_prompt(q, k, v, q_start, k_start=None, causal=True, scale=None, lse=False):
+    """Attention of packed sequences: q [n_q][n_heads][dim], k and v [n_k][n_kv_heads][dim],
+    starts q_start and k_start (q_start if None) [n + 1]: [n_q][n_heads][dim], with lse also
+    [n_q][n_heads]."""
+    k_start = q_start if k_start is None else k_start
+    q = _rows(q, "q")
+    a = cf_attn_seqs()
+    a.n_q, a.n_heads, a.head_dim = (int(x) for x in q.shape)
+    k = _rows(k, "k", None, a.head_dim, q.dtype)
+    v = _rows(v, "v", int(k.shape[1]), a.head_dim, q.dtype)
+    if v.shape[0] != k.shape[0]:
+        raise CfError("k and v: %d and %d tokens" % (k.shape[0], v.shape[0]))
+    a.n_k, a.n_kv_heads, a.n_seq = int(k.shape[0]), int(k.shape[1]), int(q_start.numel()) - 1
+    a.dtype, a.causal = ATTN_DTYPE[q.dtype], int(bool(causal))
+    q_start, k_start = q_start.contiguous(), k_start.contiguous()
+    a.q_start_dev = _in(q_start, torch.int32, "q_start", ndim=1)
+    a.k_start_dev = _in(k_start, torch.int32, "k_start", a.n_seq + 1)
+    a.q_dev, a.k_dev, a.v_dev = q.data_ptr(), k.data_ptr(), v.data_ptr()
+    a.q_tok, a.q_head, a.k_tok, a.k_head = q.stride(0), q.stride(1), k.stride(0), k.stride(1)
+    a.v_tok, a.v_head = v.stride(0), v.stride(1)
+    out = torch.empty(tuple(q.shape), dtype=q.dtype, device=q.device)
+    ls = torch.empty((a.n_q, a.n_heads), dtype=torch.float32, device=q.device) if lse else None
+    _check(_lib.cf_attn_prompt(C.byref(a), float(a.head_dim ** -0.5 if scale is None else scale), _p(out), _p(ls),
+                               _stream()), "cf_attn_prompt")
+    return (out, ls) if lse else out
 
 
 def cf_math_eval(op, x, y=None):
