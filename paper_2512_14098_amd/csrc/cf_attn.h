@@ -37,9 +37,7 @@ struct Elem<_Float16> {
 
 constexpr float kNegInf = -__builtin_inff();
 constexpr int kRowsSmall = 16;   // (token, head) rows of a workgroup of the few-row kernel
-constexpr int kRowsBig = 128;    // of the many-row kernel
-constexpr int kPartsSmall = 1024;  // workgroups the plan splits long contexts for
-constexpr int kPartsBig = 512;
+constexpr int kRowsGroup = 128;  // of a group of four waves of the many-row kernel
 constexpr int kMinPart = 256;    // fewest keys of a part of a split context
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -80,21 +78,19 @@ __device__ __forceinline__ V8 join8(V4 a, V4 b) {
 // ------------------------------------------------------------------ the plan in memory
 struct PlanHdr {
   int32_t n_items[2];  // few-row and many-row kernel
-  int32_t n_join[2];
   int32_t part[2];     // keys of a part of a split context
-  int32_t pad[10];
+  int32_t pad[12];
 };
 struct PlanItem {
-  int32_t seq, tile, lo, slot;  // slot -1: the rows' whole context, else the partial result's place
-};
-struct PlanJoin {
-  int32_t seq, tile, slot, n;
+  int32_t seq, tile, part, n;  // part of n of the context of a tile of rows
+  int32_t slot, join;          // n > 1: the tile's first partial result, its counter
+  int32_t pad[2];
 };
 struct PlanView {
   PlanHdr *hdr;
   PlanItem *items[2];
-  PlanJoin *join[2];
-  float *o[2], *ml[2];
+  int32_t *done[2];    // [split tile][key/value head]: parts finished, zero between calls
+  float *o[2], *ml[2];  // partial results: [slot][key/value head][row]
   int32_t cap_items[2], cap_slots[2], cap_join[2];
 };
 
@@ -136,8 +132,5 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs &a, int seq, int &k0) {
   }
   return r;
 }
-
-// 16 zero bytes that masked lanes load instead of a key or a value
-extern __device__ const i32x4 g_zero16;
 
 }  // namespace cf

@@ -20,14 +20,46 @@
 
 namespace cf {
 
-__device__ const i32x4 g_zero16 = {0, 0, 0, 0};
+// Zeros that lanes load in place of keys and values that are not there: 16 rows
+// of the widest head, so that a whole page group can be pointed at them.
+__device__ i32x4 g_zeros[16 * 256 * 2 / 16];
 
 bool page_ok(int page);
 cf_status check_cache(const cf_kv_cache *c);
 
 namespace {
 
+// Partial results pass between workgroups behind different L2s.  They are stored and loaded
+// 8 bytes at a time as atomics of device scope, which go past the L2s, and a workgroup says
+// that it is done after its stores have arrived: a fence would write back and drop the whole
+// L2, keys and values in flight to the other workgroups with it (few-row kernel on 256
+// requests: 886 us against 330).
+__device__ __forceinline__ void store_part(float *p, float x, float y) {
+  __hip_atomic_store((uint64_t *)p, (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_part(const float *p) {
+  const uint64_t u = __hip_atomic_load((uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32)));
+}
+__device__ __forceinline__ void parts_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Log of the sum of exponentials from the running maximum and sum, natural.
+__device__ __forceinline__ float log_sum(float m, float l, float s2) {
+  return l == 0.f ? kNegInf : (m * s2 + __log2f(l)) * 0.69314718055994531f;
+}
+
+// Most parts of one context: their weights for a tile's rows are held in LDS.
+__host__ __device__ constexpr int max_parts(int kind) { return kind ? 32 : 256; }
+
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// 16 bytes of global memory (said to the compiler, which else takes the pointer
+// for one that may be into LDS, and its loads wait on both counters).
+__device__ __forceinline__ i32x4 load16(const void *p) {
+  typedef const __attribute__((address_space(1))) i32x4 *gp;
+  return *(gp)(uintptr_t)p;
+}
 
 // Rows in LDS are DS elements (64, 128 or 256), cut into 16-byte chunks that
 // are permuted within a row by an exclusive or with a function of the row, so
@@ -46,113 +78,182 @@ __device__ __forceinline__ int swz8(int row) {
 }
 
 // ------------------------------------------------------------------ plan
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *lds) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+
+// Sums over the block of two numbers a thread.
+__device__ __forceinline__ void block_sum2(int64_t &x, int64_t &y, int64_t (*lds)[2]) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  __syncthreads();
-  if (lane == 0) lds[w] = x;
-  __syncthreads();
-  int64_t s = 0;
-  for (int i = 0; i < nw; i++) s += lds[i];
-  return s;
-}
-__device__ __forceinline__ int64_t block_before(int64_t x, int64_t *lds, int64_t &total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  int64_t incl = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(incl, o);
-    if (lane >= o) incl += y;
+  for (int o = 32; o; o >>= 1) {
+    x += __shfl_xor(x, o);
+    y += __shfl_xor(y, o);
   }
   __syncthreads();
-  if (lane == 63) lds[w] = incl;
-  __syncthreads();
-  int64_t before = incl - x;
-  total = 0;
-  for (int i = 0; i < nw; i++) {
-    if (i < w) before += lds[i];
-    total += lds[i];
+  if ((threadIdx.x & 63) == 0) {
+    lds[threadIdx.x >> 6][0] = x;
+    lds[threadIdx.x >> 6][1] = y;
   }
-  return before;
+  __syncthreads();
+  x = y = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanWaves; i++) {
+    x += lds[i][0];
+    y += lds[i][1];
+  }
 }
 
-constexpr int kPlanThreads = 1024;
+// How the contexts of one kernel's requests are split.  n workgroups run at a time per
+// key/value head; candidate c aims at 2^c parts for each of them (c = 0, 1; c < 0: no split).  A
+// candidate's time is estimated in keys: its parts in full rounds, or their sum over the
+// workgroups and half a part of tail, whichever is less, and `cost` keys for starting a
+// part and joining its result.
+struct Split {
+  int n, cost, max_parts;
+};
 
-// One workgroup.  Pass 1 sums the work of either kernel, (row tiles) x (keys),
-// which gives the keys of a part; pass 2 takes 1024 requests at a time, places
+// One workgroup.  Pass 1 sums the work of either kernel, (row tiles) x (keys), and the
+// parts that each candidate length gives; pass 2 takes 1024 requests at a time, places
 // their items by a scan and writes them, a thread per item.
 __global__ __launch_bounds__(kPlanThreads) void k_attn_plan(PlanView v, const int32_t *q_start, const int32_t *kv_len,
-                                                            int n_seq, int n_tok, int G, int Hkv, int few_only) {
-  __shared__ int64_t red[kPlanThreads / 64];
-  __shared__ int64_t l_at[kPlanThreads], l_slot[kPlanThreads], l_join[kPlanThreads];
+                                                            int n_seq, int n_tok, int G, int Hkv, int few_only,
+                                                            int big_log2, Split sp0, Split sp1) {
+  __shared__ int64_t red[kPlanWaves][2];
+  __shared__ int64_t l_at[kPlanThreads];
   __shared__ int l_n[kPlanThreads];
+  __shared__ int l_keys[2];
   const int tid = threadIdx.x;
   auto load = [&](int i, int &tiles, int &kind, int &keys) {
-    const int q0 = clampi(q_start[i], 0, n_tok), n = max(clampi(q_start[i + 1], 0, n_tok) - q0, 0);
-    const int64_t rows = (int64_t)n * G;
+    const int q0 = clampi(q_start[i], 0, n_tok), rows = max(clampi(q_start[i + 1], 0, n_tok) - q0, 0) * G;
     kind = (!few_only && rows > kRowsSmall) ? 1 : 0;
-    tiles = (int)ceil_div(rows, kind ? kRowsBig : kRowsSmall);
-    keys = max(kv_len[i], 0);
+    const int sh = kind ? big_log2 : 4;
+    tiles = (rows + (1 << sh) - 1) >> sh;
+    keys = clampi(kv_len[i], 0, 1 << 29);  // the last part of a context has no end
   };
-  int64_t w0 = 0, w1 = 0;
+  // the counters of finished parts start at zero
+  for (int k = 0; k < 2; k++)
+    for (int i = tid; i < v.cap_join[k] * Hkv; i += kPlanThreads) v.done[k][i] = 0;
+  if (tid < 2) l_keys[tid] = 0;
+  int tiles0 = 0, kind0 = 0, keys0 = 0;  // the thread's first request, kept for pass 2
+  if (tid < n_seq) load(tid, tiles0, kind0, keys0);
+  int64_t w[2] = {0, 0};
+  int longest[2] = {0, 0};
   for (int i = tid; i < n_seq; i += kPlanThreads) {
-    int tiles, kind, keys;
-    load(i, tiles, kind, keys);
-    (kind ? w1 : w0) += (int64_t)tiles * keys;
+    int tiles = tiles0, kind = kind0, keys = keys0;
+    if (i != tid) load(i, tiles, kind, keys);
+    w[kind] += (int64_t)tiles * keys;
+    if (tiles > 0) longest[kind] = max(longest[kind], keys);
   }
-  w0 = block_sum(w0, red);
-  w1 = block_sum(w1, red);
+  __syncthreads();
+  if (longest[0] > 0) atomicMax(&l_keys[0], longest[0]);
+  if (longest[1] > 0) atomicMax(&l_keys[1], longest[1]);
+  block_sum2(w[0], w[1], red);  // its barriers also cover l_keys
   int part[2];
   for (int k = 0; k < 2; k++) {
-    const int64_t target = ceil_div(k ? kPartsBig : kPartsSmall, Hkv);
-    const int64_t p = ceil_div(k ? w1 : w0, target);
-    part[k] = (int)min((int64_t)(1 << 30), ceil_div(max(p, (int64_t)kMinPart), 128) * 128);
+    const Split sp = k ? sp1 : sp0;
+    const int keys_max = l_keys[k];
+    part[k] = 0x7fffff80;
+    if (w[k] == 0) continue;
+    float best = 0.f;
+    for (int c = -1; c < 2; c += 2) {  // no split beside one part each; two parts each
+      int len[2];
+      int64_t n[2] = {0, 0};
+      for (int e = 0; e < 2; e++) {
+        // at least the even share, so the parts of split contexts number less than 2 x 2 x n;
+        // the sum is in doubles: an estimate, then one more
+        const double even = c + e < 0 ? 0x1p30 : (double)w[k] / ((double)sp.n * (1 << min(c + e, 1))) + 1.0;
+        const int floor_len = max(kMinPart, keys_max / sp.max_parts + 1);
+        len[e] = (max((int)fmin(even, 0x1p30), floor_len) + 127) & ~127;
+      }
+      for (int i = tid; i < n_seq; i += kPlanThreads) {
+        int tiles = tiles0, kind = kind0, keys = keys0;
+        if (i != tid) load(i, tiles, kind, keys);
+        if (kind != k) continue;
+        n[0] += (int64_t)tiles * max((int)((unsigned)(keys + (unsigned)len[0] - 1u) / (unsigned)len[0]), 1);
+        n[1] += (int64_t)tiles * max((int)((unsigned)(keys + (unsigned)len[1] - 1u) / (unsigned)len[1]), 1);
+      }
+      block_sum2(n[0], n[1], red);
+      for (int e = 0; e < 2; e++) {
+        const float most = (float)min(len[e], keys_max), per = (float)n[e] / sp.n;
+        const float t = fminf(ceilf(per) * most, fmaxf((float)w[k] / sp.n, most) + 0.5f * most) + per * sp.cost;
+        if ((c < 0 && e == 0) || t < best) {
+          best = t;
+          part[k] = len[e];
+        }
+      }
+    }
   }
-  // 64-bit: starts that do not ascend could name more rows than there are
-  int64_t at[2] = {0, 0}, slots[2] = {0, 0}, joins[2] = {0, 0};
+  // Items (40 bits), parts of split contexts (12) and split tiles (12) are placed by one scan:
+  // the last two are bounded by the choice of the part whatever the lengths are.
+  int64_t at[2] = {0, 0};
+  int slots[2] = {0, 0}, joins[2] = {0, 0};
   for (int c0 = 0; c0 < n_seq; c0 += kPlanThreads) {
     const int i = c0 + tid, cn = min(kPlanThreads, n_seq - c0);
-    int tiles = 0, kind = 0, keys = 0, parts = 1;
-    if (i < n_seq) {
-      load(i, tiles, kind, keys);
-      parts = max((int)ceil_div(keys, part[kind]), 1);
-    }
+    int tiles = c0 ? 0 : tiles0, kind = c0 ? 0 : kind0, keys = c0 ? 0 : keys0;
+    if (c0 && i < n_seq) load(i, tiles, kind, keys);
+    const int parts = max((int)((unsigned)(keys + (unsigned)part[kind] - 1u) / (unsigned)part[kind]), 1);
     for (int k = 0; k < 2; k++) {
+      if (k && few_only) break;
       const bool mine = kind == k && tiles > 0;
       const int64_t items = mine ? (int64_t)tiles * parts : 0;
-      int64_t n, ns, nj;
-      l_n[tid] = mine ? parts : 0;
-      l_at[tid] = block_before(items, red, n);
-      l_slot[tid] = block_before(parts > 1 ? items : 0, red, ns);
-      l_join[tid] = block_before(mine && parts > 1 ? tiles : 0, red, nj);
-      __syncthreads();
-      const int64_t room = v.cap_items[k] - at[k];
-      for (int64_t x = tid; x < min(n, room); x += kPlanThreads) {
-        int lo = 0, hi = cn;  // the last request with items that starts at or before item x
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (l_at[mid] <= x) lo = mid; else hi = mid;
-        }
-        const int p = max(l_n[lo], 1);
-        const int64_t rest = x - l_at[lo];
-        const int tile = (int)(rest / p), pi = (int)(rest - (int64_t)tile * p);
-        const int64_t slot = p > 1 ? slots[k] + l_slot[lo] + rest : -1;
-        const int64_t join = joins[k] + l_join[lo] + tile;
-        if (slot + p > v.cap_slots[k] + pi) continue;
-        v.items[k][at[k] + x] = PlanItem{c0 + lo, tile, pi * part[k], (int)slot};
-        if (p > 1 && pi == 0 && join < v.cap_join[k]) v.join[k][join] = PlanJoin{c0 + lo, tile, (int)slot, p};
+      const int64_t x = items | (parts > 1 ? (items << 40) | ((int64_t)(mine ? tiles : 0) << 52) : 0);
+      // running sums over the block
+      const int lane = tid & 63, wv = tid >> 6;
+      int64_t incl = x;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int64_t y = __shfl_up(incl, o);
+        if (lane >= o) incl += y;
       }
       __syncthreads();
-      at[k] += n; slots[k] += ns; joins[k] += nj;
+      if (lane == 63) red[wv][0] = incl;
+      l_n[tid] = mine ? parts : 0;
+      __syncthreads();
+      int64_t before = incl - x, total = 0;
+#pragma unroll
+      for (int e = 0; e < kPlanWaves; e++) {
+        if (e < wv) before += red[e][0];
+        total += red[e][0];
+      }
+      l_at[tid] = before;
+      __syncthreads();
+      const int64_t low = (1ll << 40) - 1;
+      const int64_t n = total & low, room = v.cap_items[k] - at[k];
+      for (int64_t y = tid; y < min(n, room); y += kPlanThreads) {
+        int lo = 0, hi = cn;  // the last request with items that starts at or before item y
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if ((l_at[mid] & low) <= y) lo = mid; else hi = mid;
+        }
+        const int64_t b = l_at[lo];
+        const unsigned np = (unsigned)max(l_n[lo], 1), rest = (unsigned)(y - (b & low));
+        const int tile = (int)(rest / np), pi = (int)(rest - tile * np);
+        PlanItem it = {c0 + lo, tile, pi, (int)np, -1, -1, {0, 0}};
+        if (np > 1) {
+          it.slot = slots[k] + (int)((uint64_t)b >> 40 & 0xfff) + tile * (int)np;
+          it.join = joins[k] + (int)((uint64_t)b >> 52) + tile;
+        }
+        v.items[k][at[k] + y] = it;
+      }
+      at[k] += n;
+      slots[k] += (int)((uint64_t)total >> 40 & 0xfff);
+      joins[k] += (int)((uint64_t)total >> 52);
     }
   }
   if (tid < 2) {
     v.hdr->n_items[tid] = (int)min(at[tid], (int64_t)v.cap_items[tid]);
-    v.hdr->n_join[tid] = (int)min(joins[tid], (int64_t)v.cap_join[tid]);
     v.hdr->part[tid] = part[tid];
   }
 }
+
+struct Dyn {
+  int value;
+};
+// The kernels' state is held by reference in lambdas: not inlined, it would be memory.
+#define CF_INLINE __attribute__((always_inline))
+
+template <int N>
+struct Int {
+  static constexpr int value = N;
+};
 
 // Infinities and NaN: exponent all ones.
 template <typename T>
@@ -179,36 +280,118 @@ __device__ __forceinline__ bool special(T x) {
 // The infinities and NaN among the values of keys [from, to), which only some
 // of the rows row0 .. row0 + n - 1 see, added to the results just written.
 template <typename T, bool PAGED>
-__device__ __forceinline__ void add_specials(const AttnArgs &a, const Rows &r, int k0, int seq, int slot, int kind,
-                                             int head, int64_t row0, int n, int from, int to) {
+__device__ __forceinline__ void add_specials(const AttnArgs &a, const Rows &r, int k0, int seq, int slot, int R,
+                                             int head, int row0, int n, int from, int to) {
+  parts_arrived();
   __syncthreads();
 #pragma unroll 1
-  for (int x = threadIdx.x; x < n * a.D; x += 256) {
-    const int rr = x / a.D, e = x - rr * a.D;
-    const int64_t row = row0 + rr;
-    const int j = (int)(row / a.G), g = (int)(row - (int64_t)j * a.G);
+  for (int x = threadIdx.x; x < n * (a.D / 2); x += (int)blockDim.x) {
+    const int rr = x / (a.D / 2), e = (x - rr * (a.D / 2)) * 2;
+    const int row = row0 + rr, j = row / a.G, g = row - j * a.G;
     const int last = min(r.nk - r.nq + j, to - 1);
-    float sum = 0.f;
+    float sum[2] = {0.f, 0.f};
 #pragma unroll 1
     for (int key = from; key <= last; key++) {
-      T v = (T)0.f;
+      const T *v = (const T *)g_zeros;
       if (PAGED) {
         const int id = a.table[(int64_t)seq * a.max_pages + (key >> a.page_log2)];
         if ((unsigned)id < (unsigned)a.n_pages)
-          v = ((const T *)a.v)[((((int64_t)id * a.Hkv + head) << a.page_log2) + (key & ((1 << a.page_log2) - 1))) * a.D + e];
+          v = (const T *)a.v + ((((int64_t)id * a.Hkv + head) << a.page_log2) + (key & ((1 << a.page_log2) - 1))) * a.D + e;
       } else {
-        v = ((const T *)a.v)[(int64_t)(k0 + key) * a.v_tok + head * a.v_head + e];
+        v = (const T *)a.v + (int64_t)(k0 + key) * a.v_tok + head * a.v_head + e;
       }
-      if (special<T>(v)) sum += (float)v;
+      if (special<T>(v[0])) sum[0] += (float)v[0];
+      if (special<T>(v[1])) sum[1] += (float)v[1];
     }
-    if (sum == 0.f) continue;
+    if (sum[0] == 0.f && sum[1] == 0.f) continue;
     if (slot >= 0) {
-      const int R = kind ? kRowsBig : kRowsSmall;
-      a.plan.o[kind][(((int64_t)slot * a.Hkv + head) * R + rr) * a.D + e] += sum;
+      float *p = a.plan.o[R > kRowsSmall] + (((int64_t)slot * a.Hkv + head) * R + rr) * a.D + e;
+      const float2 o = load_part(p);
+      store_part(p, o.x + sum[0], o.y + sum[1]);
     } else {
       T *p = (T *)a.out + ((int64_t)(r.q0 + j) * a.H + head * a.G + g) * a.D + e;
-      *p = (T)((float)*p + sum);
+      p[0] = (T)((float)p[0] + sum[0]);
+      p[1] = (T)((float)p[1] + sum[1]);
     }
+  }
+}
+
+// ------------------------------------------------------------------ work items
+struct Item {
+  int seq, tile, part, n, slot, join;  // part of n of the rows' context; n 1: slot and join unused
+  int lo, end;                         // its keys
+};
+
+// Item `item` of the plan, if there is one and it names what exists.
+__device__ __forceinline__ bool read_item(const AttnArgs &a, int kind, int item, Item &it) {
+  if (item >= min(a.plan.hdr->n_items[kind], a.plan.cap_items[kind])) return false;
+  const PlanItem p = a.plan.items[kind][item];
+  const int len = a.plan.hdr->part[kind];
+  it = Item{p.seq, p.tile, p.part, p.n, p.slot, p.join, 0, 0x7fffffff};
+  if ((unsigned)p.seq >= (unsigned)a.n_seq || p.tile < 0 || p.n < 1) return false;
+  if (p.n > 1) {
+    if (p.part < 0 || p.part >= p.n || p.slot < 0 || p.slot > a.plan.cap_slots[kind] - p.n ||
+        (unsigned)p.join >= (unsigned)a.plan.cap_join[kind] || p.n > max_parts(kind) || len < 1 || len >= 1 << 30)
+      return false;
+    it.lo = (int)min((int64_t)p.part * len, (int64_t)1 << 30);
+    if (p.part < p.n - 1) it.end = it.lo + len;
+  }
+  return true;
+}
+
+// The parts of a split context are joined by the workgroup that finishes last, in part
+// order whichever it is:  m = max m_p, l = sum l_p e^(m_p - m), o = sum o_p e^(m_p - m) / l.
+// w: LDS of this workgroup, at least max_parts x R floats and 4 per thread.
+template <typename T, int R>
+__device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, const Item &it, int head, int row0,
+                                           int n, float *w) {
+  using V4 = typename Elem<T>::v4;
+  constexpr int kind = R > kRowsSmall;
+  __shared__ int last;
+  __shared__ float l_sum[R];
+  const int tid = threadIdx.x, nt = (int)blockDim.x;
+  parts_arrived();
+  __syncthreads();
+  if (tid == 0) {
+    int *done = a.plan.done[kind] + (int64_t)it.join * a.Hkv + head;
+    last = atomicAdd(done, 1) == it.n - 1;
+    if (last) *done = 0;  // for the next layer's call
+  }
+  __syncthreads();
+  if (!last) return;
+  const float *ml = a.plan.ml[kind], *o = a.plan.o[kind];
+  const int64_t base = ((int64_t)it.slot * a.Hkv + head) * R, step = (int64_t)a.Hkv * R;
+  // a row's weights of the parts; lse
+  for (int rr = tid; rr < n; rr += nt) {
+    float m = kNegInf, l = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < it.n; p++) m = fmaxf(m, load_part(ml + (base + p * step + rr) * 2).x);
+    const float mu = m == kNegInf ? 0.f : m;
+#pragma unroll 4
+    for (int p = 0; p < it.n; p++) {
+      const float2 x = load_part(ml + (base + p * step + rr) * 2);
+      const float f = exp2_hw((x.x - mu) * a.s2);
+      w[p * R + rr] = f;
+      l = fmaf(f, x.y, l);
+    }
+    l_sum[rr] = l > 0.f || l != l ? 1.f / l : 0.f;
+    const int j = (row0 + rr) / a.G, g = row0 + rr - j * a.G;
+    if (a.lse) a.lse[(int64_t)(r.q0 + j) * a.H + head * a.G + g] = log_sum(m, l, a.s2);
+  }
+  __syncthreads();
+  const int quads = a.D / 4;
+  for (int x = tid; x < n * quads; x += nt) {
+    const int rr = x / quads, d4 = x - rr * quads;
+    f32x4 acc = {0, 0, 0, 0};
+#pragma unroll 8
+    for (int p = 0; p < it.n; p++) {
+      const float *src = o + (base + p * step + rr) * a.D + d4 * 4;
+      const float2 x = load_part(src), y = load_part(src + 2);
+      acc += f32x4{x.x, x.y, y.x, y.y} * w[p * R + rr];
+    }
+    const int j = (row0 + rr) / a.G, g = row0 + rr - j * a.G;
+    T *out = (T *)a.out + ((int64_t)(r.q0 + j) * a.H + head * a.G + g) * a.D + d4 * 4;
+    *(V4 *)out = __builtin_convertvector(acc * l_sum[rr], V4);
   }
 }
 
@@ -230,9 +413,8 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
   __shared__ float l_m[4][16], l_l[4][16];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = (int)(blockIdx.x % (unsigned)a.Hkv), item = (int)(blockIdx.x / (unsigned)a.Hkv);
-  if (item >= min(a.plan.hdr->n_items[0], a.plan.cap_items[0])) return;
-  const PlanItem it = a.plan.items[0][item];
-  if ((unsigned)it.seq >= (unsigned)a.n_seq || it.tile < 0 || it.lo < 0 || it.slot >= a.plan.cap_slots[0]) return;
+  Item it;
+  if (!read_item(a, 0, item, it)) return;
   int k0;
   const Rows r = rows_of<true>(a, it.seq, k0);
   const int n_rows = r.nq * a.G, row0 = it.tile * kRowsSmall;
@@ -240,8 +422,7 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
   const int row = row0 + (lane & 15), j = min(row, n_rows - 1) / a.G, g = min(row, n_rows - 1) - j * a.G;
   const int last_j = (min(row0 + kRowsSmall, n_rows) - 1) / a.G;
   const int seen = r.nk - r.nq + last_j + 1;  // keys the tile's last row sees
-  const int hi = __builtin_amdgcn_readfirstlane(
-      min(seen, it.slot >= 0 ? it.lo + a.plan.hdr->part[0] : 0x7fffffff));
+  const int hi = __builtin_amdgcn_readfirstlane(min(seen, it.end));
   const int lim = r.nk - r.nq + j;  // last key the lane's row sees
   const int all = r.nk - r.nq + row0 / a.G + 1;  // keys that every row sees
 
@@ -251,7 +432,7 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
 #pragma unroll
   for (int ks = 0; ks < KS; ks++) {
     const int c = ks * 4 + gq;
-    qf[ks] = *(const V8 *)(c * 8 < a.D ? (const void *)(qp + c * 8) : (const void *)&g_zero16);
+    qf[ks] = __builtin_bit_cast(V8, load16(c * 8 < a.D ? (const void *)(qp + c * 8) : (const void *)g_zeros));
   }
 
   const int64_t page_elems = (int64_t)a.Hkv * a.D << a.page_log2;
@@ -294,13 +475,13 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
       for (int ks = 0; ks < KS; ks++) {
         const int c = ks * 4 + gq, key = lane & 15;
         const bool ok = key < valid[b] && c * 8 < a.D;
-        kr[b][ks] = *(const V8 *)(ok ? (const void *)(kc + base[b] + key * a.D + c * 8) : (const void *)&g_zero16);
+        kr[b][ks] = __builtin_bit_cast(V8, load16(ok ? (const void *)(kc + base[b] + key * a.D + c * 8) : (const void *)g_zeros));
       }
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       const int x = i * 64 + lane, key = x / CH, c = x % CH, b = (i * 64 / CH) >> 4;
       const bool ok = (key & 15) < valid[b] && c * 8 < a.D;
-      vr[i] = *(const i32x4 *)(ok ? (const void *)(vc + base[b] + (key & 15) * a.D + c * 8) : (const void *)&g_zero16);
+      vr[i] = load16(ok ? (const void *)(vc + base[b] + (key & 15) * a.D + c * 8) : (const void *)g_zeros);
     }
   };
 
@@ -385,82 +566,113 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
       ll = fmaf(f, l_l[i][rr], ll);
       oo += *(const f32x4 *)((const float *)lds[i] + rr * DS + d4 * 4) * f;
     }
-    if (it.slot >= 0) {
-      const int64_t pr = ((int64_t)it.slot * a.Hkv + head) * kRowsSmall + rr;
-      *(f32x4 *)(a.plan.o[0] + pr * a.D + d4 * 4) = oo;
-      if (d4 == 0) { a.plan.ml[0][pr * 2] = mm; a.plan.ml[0][pr * 2 + 1] = ll; }
+    if (it.n > 1) {
+      const int64_t pr = ((int64_t)(it.slot + it.part) * a.Hkv + head) * kRowsSmall + rr;
+      store_part(a.plan.o[0] + pr * a.D + d4 * 4, oo[0], oo[1]);
+      store_part(a.plan.o[0] + pr * a.D + d4 * 4 + 2, oo[2], oo[3]);
+      if (d4 == 0) store_part(a.plan.ml[0] + pr * 2, mm, ll);
     } else {
       const int jj = (row0 + rr) / a.G, gg = row0 + rr - jj * a.G;
       const int64_t orow = (int64_t)(r.q0 + jj) * a.H + head * a.G + gg;
       const float inv = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
       *(V4 *)((T *)a.out + orow * a.D + d4 * 4) = __builtin_convertvector(oo * inv, V4);
-      if (a.lse && d4 == 0) a.lse[orow] = ll == 0.f ? kNegInf : (mm * a.s2 + __log2f(ll)) * 0.69314718055994531f;
+      if (a.lse && d4 == 0) a.lse[orow] = log_sum(mm, ll, a.s2);
     }
   }
   if (any_bad)
-    add_specials<T, true>(a, r, 0, it.seq, it.slot, 0, head, row0, min(n_rows - row0, kRowsSmall),
+    add_specials<T, true>(a, r, 0, it.seq, it.n > 1 ? it.slot + it.part : -1, kRowsSmall, head, row0, min(n_rows - row0, kRowsSmall),
                           it.lo + (max(all - it.lo, 0) & ~31), hi);
+  if (it.n > 1) join_parts<T, kRowsSmall>(a, r, it, head, row0, min(n_rows - row0, kRowsSmall), (float *)lds[0]);
+}
+
+// The order of a matrix phase for the instruction scheduler: NK products with one
+// operand read from LDS each, then NV with two reads each; reads run AHEAD products
+// in front, so that a product's operands have arrived when the unit is free for it.
+template <int NK, int NV, int AHEAD>
+__device__ __forceinline__ void matrix_order() {
+  constexpr int MFMA = 0x8, DSREAD = 0x100;
+  __builtin_amdgcn_sched_group_barrier(DSREAD, NK > 0 ? AHEAD : 2 * AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < NK - AHEAD; i++) {
+    __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(DSREAD, 1, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < (NK > 0 ? NV : NV - AHEAD); i++) {
+    __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(DSREAD, 2, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(MFMA, AHEAD, 0);
 }
 
 // ------------------------------------------------------------------ many rows
-// A workgroup of four waves takes 128 rows of one key/value head, 32 a wave,
-// and tiles of 64 keys.  Keys and values go through registers to LDS, the next
-// tile's loads in flight while one is worked on.  S^T = K Q^T (32 keys x 32
-// rows a matrix instruction), so a lane has 32 scores of one row, and O^T =
-// V^T P^T as in the few-row kernel: the order of the keys within a step is the
-// order in which S^T leaves them in the lane, the values' operand is read to
-// match, and no probability changes lanes.
-template <typename T, int KS, int DB, int DS, bool PAGED>
-__global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_many(AttnArgs a) {
+// A workgroup takes NG groups of four waves; a group takes 128 rows of one
+// key/value head, 32 a wave, and all share tiles of 64 keys in LDS.  S^T = K Q^T
+// (32 keys x 32 rows a matrix instruction), so a lane has 32 scores of one row,
+// and O^T = V^T P^T as in the few-row kernel: the order of the keys within a step
+// is the order in which S^T leaves them in the lane, the values' operand is read
+// to match, and no probability changes lanes.
+//
+// A wave alternates between a matrix phase, S of tile n and O += V P of tile
+// n - 1, and a vector phase, the softmax of tile n.  The two groups are one phase
+// apart: on every SIMD one wave feeds the matrix unit while the other one
+// exponentiates.  A barrier ends each phase, and with phases numbered 0, 1, 2, ...
+// group g has its matrix phase n at 2n + g.  In its vector phase n it stores its
+// share of keys n + 1 + g and values n + g, loaded one round earlier: those go to
+// the LDS halves of keys n - 1 + g and values n - 2 + g, which both groups have
+// read by then, and are complete when group 0 begins its matrix phase n + 1 + g.
+template <typename T, int KS, int DB, int DS, int NG, bool PAGED>
+__global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_attn_many(AttnArgs a) {
   using V8 = typename Elem<T>::v8;
   using V4 = typename Elem<T>::v4;
-  constexpr int CH = DS / 8, NL = 64 * CH / 256;
-  __shared__ __attribute__((aligned(16))) T lds[2][2][64 * DS];
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int NT = 256 * NG, R = kRowsGroup * NG, CH = DS / 8, NL = 64 * CH / NT, RS = NT / CH;
+  __shared__ __attribute__((aligned(16))) T lds_k[2][64 * DS], lds_v[2][64 * DS];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), grp = NG > 1 ? w >> 2 : 0;
   const int head = (int)(blockIdx.x % (unsigned)a.Hkv), item = (int)(blockIdx.x / (unsigned)a.Hkv);
-  PlanItem it;
+  Item it;
+  Rows r;
+  int k0 = 0;
   if (PAGED) {
-    if (item >= min(a.plan.hdr->n_items[1], a.plan.cap_items[1])) return;
-    it = a.plan.items[1][item];
-    if ((unsigned)it.seq >= (unsigned)a.n_seq || it.tile < 0 || it.lo < 0 || it.slot >= a.plan.cap_slots[1]) return;
+    if (!read_item(a, 1, item, it)) return;
+    r = rows_of<true>(a, it.seq, k0);
   } else {
-    // sequence i owns the tiles from floor(first row / 128) + i on; 64 probes at a time
-    auto start = [&](int i) { return (int)((int64_t)clampi(a.q_start[i], 0, a.n_tok) * a.G / kRowsBig) + i; };
-    int lo = 0, n = a.n_seq;
-    while (n > 1) {
-      const int step = (n + 63) >> 6, i = lo + lane * step;
-      const bool le = lane * step < n && start(i) <= item;
-      const int cnt = __builtin_popcountll(__ballot(le));
-      const int skip = cnt > 0 ? (cnt - 1) * step : 0;
-      lo += skip;
-      n = min(step, n - skip);
+    // sequence i owns the tiles from floor(first row / R) + i on; 64 probes at a time, the
+    // last round of them over neighbours
+    int lo = 0, n = a.n_seq, q = 0;
+    for (;;) {
+      const int step = (n + 63) >> 6;
+      q = clampi(a.q_start[lo + min(lane * step, n - 1)], 0, a.n_tok);
+      const bool le = lane * step < n && (int)((unsigned)(q * a.G) / R) + lo + lane * step <= item;
+      const int cnt = __builtin_popcountll(__ballot(le)), at = max(cnt - 1, 0);
+      q = __builtin_amdgcn_readlane(q, at);
+      lo += at * step;
+      if (step == 1) break;
+      n = min(step, n - at * step);
     }
-    it.seq = __builtin_amdgcn_readfirstlane(lo);
-    it.tile = item - __builtin_amdgcn_readfirstlane(start(lo));
+    it.seq = lo;
+    it.tile = item - ((int)((unsigned)(q * a.G) / R) + lo);
     it.lo = 0;
-    it.slot = -1;
+    it.end = 0x7fffffff;
+    it.n = 1;
+    r = rows_of<false>(a, lo, k0);
   }
-  int k0;
-  const Rows r = rows_of<PAGED>(a, it.seq, k0);
-  const int64_t n_rows = (int64_t)r.nq * a.G;
-  const int n_rt = (int)ceil_div(n_rows, kRowsBig);
+  const int n_rows = __builtin_amdgcn_readfirstlane(r.nq * a.G);  // below 2^31, as all row numbers
+  const int n_rt = (n_rows + R - 1) / R;
   if (it.tile < 0 || it.tile >= n_rt) return;
   // the rows that see most keys first
-  const int64_t row0 = (int64_t)(n_rt - 1 - it.tile) * kRowsBig;
-  const int64_t row = row0 + w * 32 + (lane & 31);
-  const int64_t rc = min(row, n_rows - 1);
-  const int j = (int)(rc / a.G), g = (int)(rc - (int64_t)j * a.G);
-  const int off = (PAGED || a.causal) ? r.nk - r.nq : r.nk;  // row j sees keys up to off + j, or all
-  const int last_j = (int)((min(row0 + kRowsBig, n_rows) - 1) / a.G);
-  const int seen = (PAGED || a.causal) ? min(off + last_j + 1, r.nk) : r.nk;
-  const int hi = __builtin_amdgcn_readfirstlane(
-      min(seen, it.slot >= 0 ? it.lo + a.plan.hdr->part[1] : 0x7fffffff));
-  const int lim = min((PAGED || a.causal) ? off + j : r.nk - 1, hi - 1);
-  // keys that every row of the wave sees need no mask
-  const int64_t wrow = min(row0 + w * 32, n_rows - 1);
-  const int all = __builtin_amdgcn_readfirstlane(
-      min((PAGED || a.causal) ? off + (int)(wrow / a.G) + 1 : r.nk, hi));
-  const int all_wg = (PAGED || a.causal) ? off + (int)(row0 / a.G) + 1 : r.nk;  // and of the workgroup
+  const int row0 = (n_rt - 1 - it.tile) * R;
+  const int row = row0 + w * 32 + (lane & 31);
+  const unsigned G = (unsigned)a.G;
+  const int j = (int)((unsigned)min(row, n_rows - 1) / G), g = min(row, n_rows - 1) - j * a.G;
+  const bool causal = PAGED || a.causal;
+  const int off = causal ? r.nk - r.nq : r.nk;  // row j sees keys up to off + j, or all
+  const int last_j = (int)((unsigned)(min(row0 + R, n_rows) - 1) / G);
+  const int seen = causal ? min(off + last_j + 1, r.nk) : r.nk;
+  const int hi = __builtin_amdgcn_readfirstlane(min(seen, it.end));
+  const int lim = min(causal ? off + j : r.nk - 1, hi - 1);
+  // keys that every row of the workgroup sees, and every row of the wave
+  const int all_wg = causal ? off + (int)((unsigned)row0 / G) + 1 : r.nk;
+  const int all = min(causal ? off + __builtin_amdgcn_readlane(j, 0) + 1 : r.nk, hi);
   const int h = lane >> 5;
 
   V8 qf[KS];
@@ -468,7 +680,7 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_many(AttnArgs a)
 #pragma unroll
   for (int ks = 0; ks < KS; ks++) {
     const int c = ks * 2 + h;
-    qf[ks] = *(const V8 *)(c * 8 < a.D ? (const void *)(qp + c * 8) : (const void *)&g_zero16);
+    qf[ks] = __builtin_bit_cast(V8, load16(c * 8 < a.D ? (const void *)(qp + c * 8) : (const void *)g_zeros));
   }
 
   const int64_t page_elems = (int64_t)a.Hkv * a.D << a.page_log2;
@@ -479,86 +691,110 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_many(AttnArgs a)
   const int32_t *trow = PAGED ? a.table + (int64_t)it.seq * a.max_pages : nullptr;
   const int n_tiles = hi > it.lo ? (hi - it.lo + 63) >> 6 : 0;
 
-  f32x16 o[DB];
+  f32x16 o[DB], s[2];
 #pragma unroll
   for (int d = 0; d < DB; d++)
 #pragma unroll
     for (int i = 0; i < 16; i++) o[d][i] = 0.f;
+  V8 pf[4];
   float m = kNegInf, l = 0.f;
   i32x4 kr[NL], vr[NL];
+#pragma unroll
+  for (int i = 0; i < NL; i++) kr[i] = vr[i] = i32x4{0, 0, 0, 0};
   int ids = 0;
   bool bad = false;
 
-  auto load = [&](int n) {
+  // Loads of a tile's keys or values; edge: some may not be there or the tile be past the
+  // last, which gives zeros.  Chunks past head_dim are never loaded and stay zero.
+  const int lrow = tid / CH, lcol = tid % CH;
+  const bool col_ok = lcol * 8 < a.D;
+  const int to_load = min(r.nk, it.lo + 64 * n_tiles);
+  auto load_ids = [&](int n) CF_INLINE {  // page ids of tiles n .. n + 7 (n a multiple of 8), one lane per 16 keys
+    const int key = it.lo + 64 * n + 16 * (lane & 31);
+    if ((lane >> 5) == ((n >> 3) & 1)) ids = key < hi ? trow[key >> a.page_log2] : -1;
+  };
+  // packed: the lane's row of the next tile to load
+  const T *kp = kc + (int64_t)lrow * a.k_tok + lcol * 8, *vp = vc + (int64_t)lrow * a.v_tok + lcol * 8;
+  auto load = [&](i32x4 (&x)[NL], const T *src, const T *&at, int64_t tok, int n, auto edge) CF_INLINE {
     const int t0 = it.lo + 64 * n;
-    if (PAGED && (n & 15) == 0) {  // page ids of 16 tiles across the lanes, one per 16 keys
-      const int key = t0 + 16 * lane;
-      ids = key < hi ? trow[key >> a.page_log2] : -1;
-    }
+    if (!col_ok) return;
 #pragma unroll
     for (int i = 0; i < NL; i++) {
-      const int x = i * 256 + tid, rr = x / CH, c = x % CH;
-      const void *kp, *vp;
+      const int rr = i * RS + lrow;
+      const T *p;
       if (PAGED) {
-        const int grp = __builtin_amdgcn_readfirstlane(rr >> 4);
-        const int id = __builtin_amdgcn_readlane(ids, ((n & 15) << 2) + grp);
+        const int kg = __builtin_amdgcn_readfirstlane(rr >> 4);
+        const int id = __builtin_amdgcn_readlane(ids, ((n & 15) << 2) + kg);
         const bool in = (unsigned)id < (unsigned)a.n_pages;
-        const int64_t base = (in ? id : 0) * page_elems + (int64_t)((t0 + 16 * grp) & page_mask) * a.D;
-        const bool ok = in && t0 + rr < r.nk && c * 8 < a.D;
-        const int e = (rr & 15) * a.D + c * 8;
-        kp = ok ? (const void *)(kc + base + e) : (const void *)&g_zero16;
-        vp = ok ? (const void *)(vc + base + e) : (const void *)&g_zero16;
+        const int64_t base = (in ? id : 0) * page_elems + (int64_t)((t0 + 16 * kg) & page_mask) * a.D;
+        p = (in ? src + base : (const T *)g_zeros) + (unsigned)((rr & 15) * a.D + lcol * 8);
       } else {
-        const bool ok = t0 + rr < r.nk && c * 8 < a.D;
-        kp = ok ? (const void *)(kc + (int64_t)(t0 + rr) * a.k_tok + c * 8) : (const void *)&g_zero16;
-        vp = ok ? (const void *)(vc + (int64_t)(t0 + rr) * a.v_tok + c * 8) : (const void *)&g_zero16;
+        p = at + i * RS * tok;
       }
-      kr[i] = *(const i32x4 *)kp;
-      vr[i] = *(const i32x4 *)vp;
+      if (edge.value) p = t0 + rr < to_load ? p : (const T *)g_zeros;
+      x[i] = load16(p);
+    }
+    if (!PAGED) at += 64 * tok;
+  };
+  auto store = [&](const i32x4 (&x)[NL], T *dst) CF_INLINE {
+#pragma unroll
+    for (int i = 0; i < NL; i++) {
+      const int rr = i * RS + lrow;
+      *(i32x4 *)(dst + rr * DS + (lcol ^ swz<DS>(rr)) * 8) = x[i];
     }
   };
-  auto store = [&](int n) {
-    const int b = n & 1;
-    if (it.lo + 64 * (n + 1) > all_wg && seen > all_wg) {
+  // keys nk and values nk - 1 to registers, or from there to LDS
+  auto fetch = [&](int nk, auto edge) CF_INLINE {
+    if (PAGED && (nk & 7) == 0) load_ids(nk);
+    load(kr, kc, kp, a.k_tok, nk, edge);
+    load(vr, vc, vp, a.v_tok, nk - 1, edge);
+  };
+  auto put = [&](int nk, T *kd, T *vd, auto edge) CF_INLINE {
+    store(kr, kd);
+    if (edge.value && it.lo + 64 * nk > all_wg && seen > all_wg) {
+      asm volatile("");  // a branch: not worth computing for every tile
 #pragma unroll
       for (int i = 0; i < NL; i++) bad |= take_specials<T>(vr[i]);
     }
-#pragma unroll
-    for (int i = 0; i < NL; i++) {
-      const int x = i * 256 + tid, rr = x / CH, c = x % CH, at = rr * DS + (c ^ swz<DS>(rr)) * 8;
-      *(i32x4 *)(&lds[b][0][at]) = kr[i];
-      *(i32x4 *)(&lds[b][1][at]) = vr[i];
-    }
+    store(vr, vd);
   };
 
-  if (n_tiles > 0) {
-    load(0);
-    store(0);
-  }
-  __syncthreads();
-  for (int n = 0; n < n_tiles; n++) {
-    const int t0 = it.lo + 64 * n;
-    if (n + 1 < n_tiles) load(n + 1);
-    const T *kt = lds[n & 1][0], *vt = lds[n & 1][1];
-    f32x16 s[2];
+  auto scores = [&](const T *kt) CF_INLINE {
+    const int rr = lane & 31;
 #pragma unroll
-    for (int b = 0; b < 2; b++) {
+    for (int b = 0; b < 2; b++)
 #pragma unroll
       for (int i = 0; i < 16; i++) s[b][i] = 0.f;
-      const int rr = b * 32 + (lane & 31);
 #pragma unroll
-      for (int ks = 0; ks < KS; ks++) {
-        const V8 kf = *(const V8 *)(kt + rr * DS + (((ks * 2 + h) ^ swz<DS>(rr)) * 8));
+    for (int ks = 0; ks < KS; ks++)
+#pragma unroll
+      for (int b = 0; b < 2; b++) {
+        const V8 kf = *(const V8 *)(kt + b * 32 * DS + rr * DS + (((ks * 2 + h) ^ swz<DS>(rr)) * 8));
         s[b] = Elem<T>::mma32(kf, qf[ks], s[b]);
       }
-    }
-    if (t0 + 64 > all) {
+  };
+  const int vcol = 16 * ((lane >> 4) & 1) + 4 * (lane & 3), vr0 = 4 * h + ((lane & 15) >> 2);
+  auto values = [&](const T *vt) CF_INLINE {
+#pragma unroll
+    for (int k = 0; k < 4; k++)
+#pragma unroll
+      for (int d = 0; d < DB; d++) {
+        const int c = d * 4 + (vcol >> 3), of = vcol & 7;
+        const V4 lo4 = read_tr<T>(vt + k * 16 * DS + vr0 * DS + (c ^ swz<DS>(vr0)) * 8 + of);
+        const V4 hi4 = read_tr<T>(vt + k * 16 * DS + (vr0 + 8) * DS + (c ^ swz<DS>(vr0 + 8)) * 8 + of);
+        o[d] = Elem<T>::mma32(join8<V8>(lo4, hi4), pf[k], o[d]);
+      }
+  };
+  auto softmax = [&](int n, auto edge) CF_INLINE {
+    const int t0 = it.lo + 64 * n;
+    if (edge.value && t0 + 64 > all) {
+      const int room = lim - t0 - 4 * h;
+      asm volatile("");
 #pragma unroll
       for (int b = 0; b < 2; b++)
 #pragma unroll
         for (int i = 0; i < 16; i++) {
-          const int key = t0 + b * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
-          s[b][i] = key <= lim ? s[b][i] : kNegInf;
+          s[b][i] = b * 32 + 8 * (i >> 2) + (i & 3) <= room ? s[b][i] : kNegInf;
         }
     }
     float mx = kNegInf;
@@ -567,50 +803,103 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_many(AttnArgs a)
 #pragma unroll
       for (int i = 0; i < 16; i++) mx = fmaxf(mx, s[b][i]);
     mx = max_halves(mx);
-    const float mn = fmaxf(m, mx), mu = mn == kNegInf ? 0.f : mn * a.s2;
-    const float alpha = exp2_hw(fmaf(m, a.s2, -mu));
-    m = mn;
-    V8 pf[4];
-    float ps = 0.f;
+    // the maximum follows only when some row's has grown by more than 2^8 in its exponentials:
+    // p_k up to 256 do no harm, and most tiles need not scale o
+    if (__ballot((mx - m) * a.s2 > 8.f)) {
+      const float mn = fmaxf(m, mx);
+      const float alpha = mn == kNegInf ? 1.f : exp2_hw((m - mn) * a.s2);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; d++) o[d] = o[d] * alpha;
+    }
+    const float mu = m == kNegInf ? 0.f : m * a.s2;
 #pragma unroll
     for (int b = 0; b < 2; b++)
 #pragma unroll
       for (int i = 0; i < 16; i++) {
         const float p = exp2_hw(fmaf(s[b][i], a.s2, -mu));
-        ps += p;
+        l += p;
         pf[b * 2 + (i >> 3)][i & 7] = (T)p;
       }
-    l = fmaf(l, alpha, ps);
-#pragma unroll
-    for (int d = 0; d < DB; d++) o[d] = o[d] * alpha;
-    const int vcol = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    // the probabilities are made here, not where they are used, after the barrier
 #pragma unroll
     for (int k = 0; k < 4; k++) {
-      const int vrow = k * 16 + 4 * h + ((lane & 15) >> 2);
-#pragma unroll
-      for (int d = 0; d < DB; d++) {
-        const int c = d * 4 + (vcol >> 3), of = vcol & 7;
-        const V4 lo4 = read_tr<T>(vt + vrow * DS + (c ^ swz<DS>(vrow)) * 8 + of);
-        const V4 hi4 = read_tr<T>(vt + (vrow + 8) * DS + (c ^ swz<DS>(vrow + 8)) * 8 + of);
-        o[d] = Elem<T>::mma32(join8<V8>(lo4, hi4), pf[k], o[d]);
-      }
+      i32x4 x = __builtin_bit_cast(i32x4, pf[k]);
+      asm volatile("" : "+v"(x));
+      pf[k] = __builtin_bit_cast(V8, x);
     }
-    if (n + 1 < n_tiles) store(n + 1);
+  };
+
+  // One round: the matrix phase of tile n, then its vector phase.  edge: some row may not see
+  // all the keys of a tile that the round touches, or a tile not be there.
+  auto round = [&](int n, auto buf, auto edge) CF_INLINE {
+    const int B = buf.value;
+    __builtin_amdgcn_s_setprio(1);
+    scores(lds_k[B]);
+    values(lds_v[1 - B]);
+    matrix_order<2 * KS, 4 * DB, 4>();
+    __builtin_amdgcn_s_setprio(0);
+    if (NG > 1) __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+    softmax(n, edge);
+    const int q = (1 - B) ^ grp;
+    put(n + 1 + grp, lds_k[q], lds_v[1 - q], edge);
+    fetch(n + 2 + grp, edge);
+    asm volatile("" ::: "memory");  // the loads stay here, a round ahead of their store
+    __syncthreads();
+  };
+
+  // No values before the first tile's: zeros, with probabilities of zero.
+#pragma unroll
+  for (int k = 0; k < 4; k++) pf[k] = __builtin_bit_cast(V8, i32x4{0, 0, 0, 0});
+  store(vr, lds_v[1]);
+  if (PAGED) load_ids(0);
+  {
+    i32x4 first[NL];
+#pragma unroll
+    for (int i = 0; i < NL; i++) first[i] = i32x4{0, 0, 0, 0};
+    load(first, kc, kp, a.k_tok, 0, Int<1>());
+    fetch(1, Int<1>());
+    store(first, lds_k[0]);
+  }
+  __syncthreads();
+  if (grp == 1) {
+    put(1, lds_k[1], lds_v[0], Int<1>());
+    fetch(2, Int<1>());
     __syncthreads();
   }
+  // rounds whose tiles, up to the ones they fetch, every row of the workgroup sees; two at a
+  // time, one per LDS buffer
+  const int n_main = (min(all_wg, hi) - it.lo) / 64 - 1 - NG;
+  int n = 0;
+  for (; n + 2 <= n_main; n += 2) {
+    round(n, Int<0>(), Int<0>());
+    round(n + 1, Int<1>(), Int<0>());
+  }
+#pragma unroll 1
+  for (; n < n_tiles; n++) round(n, Dyn{n & 1}, Int<1>());
+  if (n_tiles > 0) {
+    values(lds_v[(n_tiles - 1) & 1]);
+    matrix_order<0, 4 * DB, 4>();
+  }
+  if (NG > 1 && grp == 0) __syncthreads();
+
   l = sum_halves(l);
   const int any_bad = __syncthreads_or(bad);
-  if (row < n_rows && it.slot >= 0) {
-    const int64_t pr = ((int64_t)it.slot * a.Hkv + head) * kRowsBig + w * 32 + (lane & 31);
+  if (row < n_rows && it.n > 1) {
+    const int64_t pr = ((int64_t)(it.slot + it.part) * a.Hkv + head) * R + w * 32 + (lane & 31);
 #pragma unroll
     for (int d = 0; d < DB; d++)
 #pragma unroll
       for (int q = 0; q < 4; q++) {
         const int e = d * 32 + 8 * q + 4 * h;
-        if (e < a.D)
-          *(f32x4 *)(a.plan.o[1] + pr * a.D + e) = f32x4{o[d][4 * q], o[d][4 * q + 1], o[d][4 * q + 2], o[d][4 * q + 3]};
+        if (e < a.D) {
+          store_part(a.plan.o[1] + pr * a.D + e, o[d][4 * q], o[d][4 * q + 1]);
+          store_part(a.plan.o[1] + pr * a.D + e + 2, o[d][4 * q + 2], o[d][4 * q + 3]);
+        }
       }
-    if (h == 0) { a.plan.ml[1][pr * 2] = m; a.plan.ml[1][pr * 2 + 1] = l; }
+    if (h == 0) store_part(a.plan.ml[1] + pr * 2, m, l);
   } else if (row < n_rows) {
     const int64_t orow = (int64_t)(r.q0 + j) * a.H + head * a.G + g;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
@@ -622,52 +911,12 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_many(AttnArgs a)
         const f32x4 x = {o[d][4 * q] * inv, o[d][4 * q + 1] * inv, o[d][4 * q + 2] * inv, o[d][4 * q + 3] * inv};
         if (e < a.D) *(V4 *)((T *)a.out + orow * a.D + e) = __builtin_convertvector(x, V4);
       }
-    if (a.lse && h == 0) a.lse[orow] = l == 0.f ? kNegInf : (m * a.s2 + __log2f(l)) * 0.69314718055994531f;
+    if (a.lse && h == 0) a.lse[orow] = log_sum(m, l, a.s2);
   }
   if (any_bad)
-    add_specials<T, PAGED>(a, r, k0, it.seq, it.slot, 1, head, row0, (int)min(n_rows - row0, (int64_t)kRowsBig),
+    add_specials<T, PAGED>(a, r, k0, it.seq, it.n > 1 ? it.slot + it.part : -1, R, head, row0, min(n_rows - row0, R),
                            it.lo + (max(all_wg - it.lo, 0) & ~63), hi);
-}
-
-// ------------------------------------------------------------------ join of split contexts
-// A workgroup per (split rows, key/value head); its parts are added in key order.
-template <typename T>
-__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int kind) {
-  using V4 = typename Elem<T>::v4;
-  const int head = (int)(blockIdx.x % (unsigned)a.Hkv), x = (int)(blockIdx.x / (unsigned)a.Hkv);
-  if (x >= min(a.plan.hdr->n_join[kind], a.plan.cap_join[kind])) return;
-  const PlanJoin jn = a.plan.join[kind][x];
-  if ((unsigned)jn.seq >= (unsigned)a.n_seq || jn.tile < 0 || jn.slot < 0 || jn.n > a.plan.cap_slots[kind] - jn.slot)
-    return;
-  const int R = kind ? kRowsBig : kRowsSmall;
-  int k0;
-  const Rows r = rows_of<true>(a, jn.seq, k0);
-  const int64_t n_rows = (int64_t)r.nq * a.G;
-  const int n_rt = (int)ceil_div(n_rows, R);
-  if (jn.tile >= n_rt) return;
-  const int64_t row0 = (int64_t)(kind ? n_rt - 1 - jn.tile : jn.tile) * R;
-  const int quads = a.D / 4;
-  for (int y = threadIdx.x; y < R * quads; y += 256) {
-    const int rr = y / quads, d4 = y - rr * quads;
-    if (row0 + rr >= n_rows) break;
-    float mm = kNegInf;
-    for (int p = 0; p < jn.n; p++)
-      mm = fmaxf(mm, a.plan.ml[kind][((((int64_t)jn.slot + p) * a.Hkv + head) * R + rr) * 2]);
-    const float mu = mm == kNegInf ? 0.f : mm;
-    float ll = 0.f;
-    f32x4 oo = {0, 0, 0, 0};
-    for (int p = 0; p < jn.n; p++) {
-      const int64_t pr = (((int64_t)jn.slot + p) * a.Hkv + head) * R + rr;
-      const float f = exp2_hw((a.plan.ml[kind][pr * 2] - mu) * a.s2);
-      ll = fmaf(f, a.plan.ml[kind][pr * 2 + 1], ll);
-      oo += *(const f32x4 *)(a.plan.o[kind] + pr * a.D + d4 * 4) * f;
-    }
-    const int j = (int)((row0 + rr) / a.G), g = (int)(row0 + rr - (int64_t)j * a.G);
-    const int64_t orow = (int64_t)(r.q0 + j) * a.H + head * a.G + g;
-    const float inv = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
-    *(V4 *)((T *)a.out + orow * a.D + d4 * 4) = __builtin_convertvector(oo * inv, V4);
-    if (a.lse && d4 == 0) a.lse[orow] = ll == 0.f ? kNegInf : (mm * a.s2 + __log2f(ll)) * 0.69314718055994531f;
-  }
+  if (PAGED && it.n > 1) join_parts<T, R>(a, r, it, head, row0, min(n_rows - row0, R), (float *)lds_k[0]);
 }
 
 // ------------------------------------------------------------------ host
@@ -688,7 +937,7 @@ cf_status check_desc(const cf_attn_desc *d) {
   if (st != CF_OK) return st;
   // row numbers are 32-bit and a grid has at most 2^24 - 1 workgroups of 256 threads
   if ((int64_t)d->n_tok * d->n_heads > 0x7fffffffll ||
-      ((int64_t)d->n_tok * d->n_heads / d->n_kv_heads / kRowsSmall + d->n_seq + 2 * kPartsSmall) * d->n_kv_heads >=
+      ((int64_t)d->n_tok * d->n_heads / d->n_kv_heads / kRowsSmall + d->n_seq + 4096) * d->n_kv_heads >=
           (1ll << 24))
     return set_error(CF_EINVAL, "n_tok x n_heads or n_seq x n_kv_heads too large");
   return CF_OK;
@@ -698,13 +947,25 @@ bool few_only(const cf_attn_desc *d) {
   return (int64_t)(d->max_new < d->n_tok ? d->max_new : d->n_tok) * (d->n_heads / d->n_kv_heads) <= kRowsSmall;
 }
 
+// The many-row kernel with two groups of four waves, out of step on one CU, or with one
+// group (two or three of its workgroups on a CU).  Two are faster on long contexts (one
+// sequence of 16384, 16 heads of 128: 1880 us against 2130), one where the work is in short
+// ones (4 x 1024, 32 heads: 64 us against 78) or too little for one workgroup of 256 rows a
+// CU (1 x 1024, 32 heads on 8: 29 us against 35); with 64 columns the exponentials outweigh
+// the products and one group is always faster, with 256 two do not fit the registers.
+int groups_of(int D, int64_t rows, int n_seq, int Hkv) {
+  return D > 64 && D <= 128 && rows >= 2048ll * n_seq && rows * Hkv >= 192 * 256 ? 2 : 1;
+}
+
 template <typename T, bool PAGED>
-void launch_many(const AttnArgs &a, int64_t blocks, hipStream_t s) {
-  const dim3 g((unsigned)blocks), b(256);
-  if (a.D <= 64) k_attn_many<T, 4, 2, 64, PAGED><<<g, b, 0, s>>>(a);
-  else if (a.D <= 96) k_attn_many<T, 6, 3, 128, PAGED><<<g, b, 0, s>>>(a);
-  else if (a.D <= 128) k_attn_many<T, 8, 4, 128, PAGED><<<g, b, 0, s>>>(a);
-  else k_attn_many<T, 16, 8, 256, PAGED><<<g, b, 0, s>>>(a);
+void launch_many(const AttnArgs &a, int groups, int64_t blocks, hipStream_t s) {
+  const dim3 g((unsigned)blocks), b((unsigned)(256 * groups));
+  if (a.D <= 64) k_attn_many<T, 4, 2, 64, 1, PAGED><<<g, b, 0, s>>>(a);
+  else if (a.D <= 96 && groups == 1) k_attn_many<T, 6, 3, 128, 1, PAGED><<<g, b, 0, s>>>(a);
+  else if (a.D <= 96) k_attn_many<T, 6, 3, 128, 2, PAGED><<<g, b, 0, s>>>(a);
+  else if (a.D <= 128 && groups == 1) k_attn_many<T, 8, 4, 128, 1, PAGED><<<g, b, 0, s>>>(a);
+  else if (a.D <= 128) k_attn_many<T, 8, 4, 128, 2, PAGED><<<g, b, 0, s>>>(a);
+  else k_attn_many<T, 16, 8, 256, 1, PAGED><<<g, b, 0, s>>>(a);
 }
 template <typename T>
 void launch_few(const AttnArgs &a, int64_t blocks, hipStream_t s) {
@@ -715,17 +976,26 @@ void launch_few(const AttnArgs &a, int64_t blocks, hipStream_t s) {
   else k_attn_few<T, 8, 16, 256><<<g, b, 0, s>>>(a);
 }
 template <typename T>
-void launch_paged(const AttnArgs &a, bool few, hipStream_t s) {
+void launch_paged(const AttnArgs &a, bool few, int groups, hipStream_t s) {
   launch_few<T>(a, (int64_t)a.plan.cap_items[0] * a.Hkv, s);
-  k_attn_join<T><<<dim3((unsigned)(a.plan.cap_join[0] * a.Hkv)), dim3(256), 0, s>>>(a, 0);
-  if (few) return;
-  launch_many<T, true>(a, (int64_t)a.plan.cap_items[1] * a.Hkv, s);
-  k_attn_join<T><<<dim3((unsigned)(a.plan.cap_join[1] * a.Hkv)), dim3(256), 0, s>>>(a, 1);
+  if (!few) launch_many<T, true>(a, groups, (int64_t)a.plan.cap_items[1] * a.Hkv, s);
 }
 
 bool scale_ok(float s) { return s > 0.f && s <= 1e38f; }
 
 }  // namespace
+
+static int desc_groups(const cf_attn_desc *d) {
+  return groups_of(d->head_dim, (int64_t)d->n_tok * (d->n_heads / d->n_kv_heads), d->n_seq, d->n_kv_heads);
+}
+
+// Workgroups of the kernels that run at a time per key/value head, as the plan counts on
+// them, and what a part costs beside its keys (measured: starting and joining one takes the
+// few-row kernel as long as 64 keys, the many-row kernel as long as 400).
+static Split split_of(const cf_attn_desc *d, int kind) {
+  const int per_cu = kind ? (desc_groups(d) > 1 || d->head_dim > 128 ? 1 : 2) : (d->head_dim > 128 ? 1 : 2);
+  return Split{(256 * per_cu + d->n_kv_heads - 1) / d->n_kv_heads, kind ? 400 : 64, max_parts(kind)};
+}
 
 uint64_t plan_view(const cf_attn_desc *d, PlanView *v) {
   const int64_t G = d->n_heads / d->n_kv_heads, rows = (int64_t)d->n_tok * G;
@@ -739,12 +1009,12 @@ uint64_t plan_view(const cf_attn_desc *d, PlanView *v) {
   };
   v->hdr = (PlanHdr *)take(sizeof(PlanHdr));
   for (int k = 0; k < 2; k++) {
-    const int R = k ? kRowsBig : kRowsSmall;
-    const int64_t parts = ceil_div(k ? kPartsBig : kPartsSmall, d->n_kv_heads);
+    const int R = k ? kRowsGroup * desc_groups(d) : kRowsSmall;
+    const int64_t parts = 2 * split_of(d, k).n;
     const int64_t with = d->n_seq < d->n_tok ? d->n_seq : d->n_tok;  // requests with new tokens
     // a request has at most floor(rows / R) + 1 tiles; with both kernels in use the few-row
     // one takes requests of one tile
-    int64_t tiles = k == 0 ? (few ? rows / R + with : with) : (few ? 0 : rows / R + with);
+    const int64_t tiles = k == 0 ? (few ? rows / R + with : with) : (few ? 0 : rows / R + with);
     const bool used = k == 0 || !few;
     // parts of a tile: ceil(keys / part) <= 1 + keys / part, and the sum of keys / part over
     // all tiles is at most `parts`; a split tile has at most 2 keys / part
@@ -752,7 +1022,7 @@ uint64_t plan_view(const cf_attn_desc *d, PlanView *v) {
     v->cap_slots[k] = used ? (int32_t)(2 * parts) : 0;
     v->cap_join[k] = used ? (int32_t)parts : 0;
     v->items[k] = (PlanItem *)take(sizeof(PlanItem) * v->cap_items[k]);
-    v->join[k] = (PlanJoin *)take(sizeof(PlanJoin) * v->cap_join[k]);
+    v->done[k] = (int32_t *)take(sizeof(int32_t) * v->cap_join[k] * d->n_kv_heads);
     const uint64_t pr = (uint64_t)v->cap_slots[k] * d->n_kv_heads * R;
     v->ml[k] = (float *)take(pr * 8);
     v->o[k] = (float *)take(pr * d->head_dim * 4);
@@ -792,7 +1062,7 @@ extern "C" cf_status cf_attn_plan(const cf_attn_desc *d, void *stream) {
   if (st != CF_OK) return st;
   k_attn_plan<<<dim3(1), dim3(kPlanThreads), 0, as_stream(stream)>>>(
       v, d->q_start_dev, d->kv_len_dev, d->n_seq, d->n_tok, d->n_heads / d->n_kv_heads, d->n_kv_heads,
-      few_only(d) ? 1 : 0);
+      few_only(d) ? 1 : 0, desc_groups(d) > 1 ? 8 : 7, split_of(d, 0), split_of(d, 1));
   return hip_check(hipGetLastError(), "cf_attn_plan");
 }
 
@@ -822,8 +1092,8 @@ extern "C" cf_status cf_attn_paged(const cf_attn_desc *d, const cf_kv_cache *cac
   a.s2 = scale * 1.44269504088896340736f;
   a.out = out_dev; a.lse = lse_dev;
   const hipStream_t s = as_stream(stream);
-  if (cache->dtype == CF_BF16) launch_paged<__bf16>(a, few_only(d), s);
-  else launch_paged<_Float16>(a, few_only(d), s);
+  if (cache->dtype == CF_BF16) launch_paged<__bf16>(a, few_only(d), desc_groups(d), s);
+  else launch_paged<_Float16>(a, few_only(d), desc_groups(d), s);
   return hip_check(hipGetLastError(), "cf_attn_paged");
 }
 
@@ -837,7 +1107,8 @@ extern "C" cf_status cf_attn_prompt(const cf_attn_seqs *p, float scale, void *ou
   if (p->dtype != CF_BF16 && p->dtype != CF_F16) return set_error(CF_EINVAL, "dtype %d", p->dtype);
   if (!scale_ok(scale)) return set_error(CF_EINVAL, "scale %g is not finite and > 0", (double)scale);
   const int64_t G = p->n_heads / p->n_kv_heads;
-  const int64_t blocks = ((int64_t)p->n_q * G / kRowsBig + p->n_seq) * p->n_kv_heads;
+  const int groups = groups_of(p->head_dim, p->n_q * G, p->n_seq, p->n_kv_heads);
+  const int64_t blocks = ((int64_t)p->n_q * G / (kRowsGroup * groups) + p->n_seq) * p->n_kv_heads;
   if ((int64_t)p->n_q * p->n_heads > 0x7fffffffll || blocks >= (1ll << 24))
     return set_error(CF_EINVAL, "n_q x n_heads or n_seq x n_kv_heads too large");
   if (p->n_q == 0) return CF_OK;
@@ -856,7 +1127,7 @@ extern "C" cf_status cf_attn_prompt(const cf_attn_seqs *p, float scale, void *ou
   a.s2 = scale * 1.44269504088896340736f;
   a.out = out_dev; a.lse = lse_dev;
   const hipStream_t s = as_stream(stream);
-  if (p->dtype == CF_BF16) launch_many<__bf16, false>(a, blocks, s);
-  else launch_many<_Float16, false>(a, blocks, s);
+  if (p->dtype == CF_BF16) launch_many<__bf16, false>(a, groups, blocks, s);
+  else launch_many<_Float16, false>(a, groups, blocks, s);
   return hip_check(hipGetLastError(), "cf_attn_prompt");
 }
