@@ -166,7 +166,8 @@ def _check(rc, what):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # the raw handle of torch's current stream: the Stream object around it costs more than a launch
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _p(t):
@@ -661,11 +662,21 @@ def _rows(t, what, heads=None, dim=None, dtype=None):
         raise CfError("%s: expected a device tensor [tokens][heads][dim]" % what)
     if t.dtype not in ATTN_DTYPE or (dtype is not None and t.dtype != dtype):
         raise CfError("%s: expected %s, got %s" % (what, dtype or "bfloat16 or float16", t.dtype))
-    if (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
+    n, h, d = t.shape
+    if (heads is not None and h != heads) or (dim is not None and d != dim):
         raise CfError("%s: expected [tokens][%s][%s], got %s" % (what, heads, dim, tuple(t.shape)))
-    if t.numel() and (t.stride(2) != 1 or t.stride(0) % 8 or t.stride(1) % 8 or t.data_ptr() % 16):
+    s0, s1, s2 = t.stride()
+    if (s2 != 1 or (s0 | s1) & 7 or t.data_ptr() & 15) and t.numel():
         t = torch.empty(tuple(t.shape), dtype=t.dtype, device=t.device).copy_(t)
     return t
+
+
+def _ints(t, what, numel=None, dtype=torch.int32):
+    """Address of a packed device tensor of integers."""
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        raise CfError("%s: expected a contiguous device tensor of %s%s, got %s %s"
+                      % (what, dtype, "" if numel is None else " x %d" % numel, t.dtype, tuple(t.shape)))
+    return t.data_ptr()
 
 
 def _kv_cache(k_cache, v_cache):
@@ -673,30 +684,30 @@ def _kv_cache(k_cache, v_cache):
         raise CfError("cache: expected two tensors [pages][heads][page][dim] of one shape and type")
     if k_cache.dtype not in ATTN_DTYPE:
         raise CfError("cache: expected bfloat16 or float16, got %s" % k_cache.dtype)
-    c = cf_kv_cache()
-    c.k_dev, c.v_dev = _p(k_cache), _p(v_cache)
-    c.n_pages, c.n_kv_heads, c.page, c.head_dim = (int(x) for x in k_cache.shape)
-    c.dtype = ATTN_DTYPE[k_cache.dtype]
-    return c
+    if not (k_cache.is_cuda and k_cache.is_contiguous() and v_cache.is_cuda and v_cache.is_contiguous()):
+        raise CfError("cache: expected contiguous device tensors")
+    pages, heads, page, dim = k_cache.shape
+    return cf_kv_cache(k_cache.data_ptr(), v_cache.data_ptr(), pages, page, heads, dim, ATTN_DTYPE[k_cache.dtype])
 
 
 def cf_kv_map(ctx_len, new_len, table, page, free_pages, head, n_tok):
     """Block tables and slot maps of one step: fills the new pages into ``table`` [n][max_pages]
     (in place) from ``free_pages``, beginning at ``head`` [1]; n_tok packed new tokens.
     Returns (q_start [n+1], kv_len [n], slots [n_tok] int64, pos [n_tok], head [1], status [n])."""
-    n, dev = int(ctx_len.numel()), ctx_len.device
-    if table.dim() != 2 or table.shape[0] != n or table.dtype != torch.int32:
+    n, n_tok = ctx_len.numel(), int(n_tok)
+    if table.dim() != 2 or table.shape[0] != n:
         raise CfError("table: expected int32 [%d][max_pages]" % n)
-    q_start = torch.empty(n + 1, dtype=torch.int32, device=dev)
-    kv_len = torch.empty(n, dtype=torch.int32, device=dev)
-    slots = torch.empty(int(n_tok), dtype=torch.int64, device=dev)
-    pos = torch.empty(int(n_tok), dtype=torch.int32, device=dev)
-    head_out = torch.empty(1, dtype=torch.int32, device=dev)
-    status = torch.empty(n, dtype=torch.int32, device=dev)
-    _check(_lib.cf_kv_map(n, _in(ctx_len, torch.int32, "ctx_len"), _in(new_len, torch.int32, "new_len", n), int(page),
-                          _p(table), int(table.shape[1]), _in(free_pages, torch.int32, "free_pages"),
-                          int(free_pages.numel()), _in(head, torch.int32, "head", 1), int(n_tok), _p(q_start),
-                          _p(kv_len), _p(slots), _p(pos), _p(head_out), _p(status), _stream()), "cf_kv_map")
+    if n_tok < 0:
+        raise CfError("n_tok %d" % n_tok)
+    # the 32-bit results are parts of one allocation
+    q_start, kv_len, pos, head_out, status = torch.empty(
+        3 * n + n_tok + 2, dtype=torch.int32, device=ctx_len.device).split((n + 1, n, n_tok, 1, n))
+    slots = torch.empty(n_tok, dtype=torch.int64, device=ctx_len.device)
+    base = q_start.data_ptr()
+    _check(_lib.cf_kv_map(n, _ints(ctx_len, "ctx_len"), _ints(new_len, "new_len", n), page, _ints(table, "table"),
+                          table.shape[1], _ints(free_pages, "free_pages"), free_pages.numel(), _ints(head, "head", 1),
+                          n_tok, base, base + 4 * (n + 1), slots.data_ptr(), base + 4 * (2 * n + 1),
+                          base + 4 * (2 * n + 1 + n_tok), base + 4 * (2 * n + 2 + n_tok), _stream()), "cf_kv_map")
     return q_start, kv_len, slots, pos, head_out, status
 
 
@@ -706,11 +717,11 @@ def cf_kv_write(k, v, k_cache, v_cache, slots):
     c = _kv_cache(k_cache, v_cache)
     k = _rows(k, "k", c.n_kv_heads, c.head_dim, k_cache.dtype)
     v = _rows(v, "v", c.n_kv_heads, c.head_dim, k_cache.dtype)
-    n = int(k.shape[0])
+    n = k.shape[0]
     if v.shape[0] != n:
         raise CfError("k and v: %d and %d tokens" % (n, v.shape[0]))
     _check(_lib.cf_kv_write(C.byref(c), n, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
-                            v.stride(1), _in(slots, torch.int64, "slots", n), _stream()), "cf_kv_write")
+                            v.stride(1), _ints(slots, "slots", n, torch.int64), _stream()), "cf_kv_write")
 
 
 class AttnPlan:
@@ -723,12 +734,9 @@ class AttnPlan:
 def cf_attn_plan(q_start, kv_len, n_tok, max_new, n_heads, n_kv_heads, head_dim):
     """The plan of one step's attention, shared by the cf_attn_paged calls of all its layers.
     max_new: the most new tokens of a request, or n_tok if not known on the host."""
-    n = int(kv_len.numel())
-    d = cf_attn_desc()
-    d.n_seq, d.n_tok, d.max_new = n, int(n_tok), int(max_new)
-    d.n_heads, d.n_kv_heads, d.head_dim = int(n_heads), int(n_kv_heads), int(head_dim)
-    q_start, kv_len = q_start.contiguous(), kv_len.contiguous()
-    d.q_start_dev, d.kv_len_dev = _in(q_start, torch.int32, "q_start", n + 1), _in(kv_len, torch.int32, "kv_len")
+    n = kv_len.numel()
+    d = cf_attn_desc(n, int(n_tok), int(max_new), int(n_heads), int(n_kv_heads), int(head_dim),
+                     _ints(q_start, "q_start", n + 1), _ints(kv_len, "kv_len"), None, 0)
     need = C.c_uint64(0)
     _check(_lib.cf_attn_plan_bytes(C.byref(d), C.byref(need)), "cf_attn_plan_bytes")
     work = torch.empty(need.value, dtype=torch.uint8, device=kv_len.device)
@@ -758,13 +766,11 @@ def cf_attn_paged(plan, q, k_cache, v_cache, table, scale=None, lse=False):
         raise CfError("q: expected %d tokens, got %d" % (d.n_tok, q.shape[0]))
     if table.dim() != 2 or table.shape[0] != d.n_seq:
         raise CfError("table: expected [%d][max_pages]" % d.n_seq)
-    table = table.contiguous()
-    out = torch.empty(tuple(q.shape), dtype=q.dtype, device=q.device)
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     ls = torch.empty((d.n_tok, d.n_heads), dtype=torch.float32, device=q.device) if lse else None
-    _check(_lib.cf_attn_paged(C.byref(d), C.byref(c), _in(table, torch.int32, "table"), int(table.shape[1]),
-                              q.data_ptr(), q.stride(0), q.stride(1),
-                              float(d.head_dim ** -0.5 if scale is None else scale), _p(out), _p(ls), _stream()),
-           "cf_attn_paged")
+    _check(_lib.cf_attn_paged(C.byref(d), C.byref(c), _ints(table, "table"), table.shape[1], q.data_ptr(), q.stride(0),
+                              q.stride(1), d.head_dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
+                              ls.data_ptr() if lse else None, _stream()), "cf_attn_paged")
     return (out, ls) if lse else out
 
 
@@ -774,24 +780,20 @@ def cf_attn_prompt(q, k, v, q_start, k_start=None, causal=True, scale=None, lse=
     [n_q][n_heads]."""
     k_start = q_start if k_start is None else k_start
     q = _rows(q, "q")
-    a = cf_attn_seqs()
-    a.n_q, a.n_heads, a.head_dim = (int(x) for x in q.shape)
-    k = _rows(k, "k", None, a.head_dim, q.dtype)
-    v = _rows(v, "v", int(k.shape[1]), a.head_dim, q.dtype)
-    if v.shape[0] != k.shape[0]:
-        raise CfError("k and v: %d and %d tokens" % (k.shape[0], v.shape[0]))
-    a.n_k, a.n_kv_heads, a.n_seq = int(k.shape[0]), int(k.shape[1]), int(q_start.numel()) - 1
-    a.dtype, a.causal = ATTN_DTYPE[q.dtype], int(bool(causal))
-    q_start, k_start = q_start.contiguous(), k_start.contiguous()
-    a.q_start_dev = _in(q_start, torch.int32, "q_start", ndim=1)
-    a.k_start_dev = _in(k_start, torch.int32, "k_start", a.n_seq + 1)
-    a.q_dev, a.k_dev, a.v_dev = q.data_ptr(), k.data_ptr(), v.data_ptr()
-    a.q_tok, a.q_head, a.k_tok, a.k_head = q.stride(0), q.stride(1), k.stride(0), k.stride(1)
-    a.v_tok, a.v_head = v.stride(0), v.stride(1)
-    out = torch.empty(tuple(q.shape), dtype=q.dtype, device=q.device)
-    ls = torch.empty((a.n_q, a.n_heads), dtype=torch.float32, device=q.device) if lse else None
-    _check(_lib.cf_attn_prompt(C.byref(a), float(a.head_dim ** -0.5 if scale is None else scale), _p(out), _p(ls),
-                               _stream()), "cf_attn_prompt")
+    n_q, heads, dim = q.shape
+    k = _rows(k, "k", None, dim, q.dtype)
+    n_k, kv_heads, _ = k.shape
+    v = _rows(v, "v", kv_heads, dim, q.dtype)
+    if v.shape[0] != n_k:
+        raise CfError("k and v: %d and %d tokens" % (n_k, v.shape[0]))
+    n_seq = q_start.numel() - 1
+    a = cf_attn_seqs(n_seq, n_q, n_k, heads, kv_heads, dim, ATTN_DTYPE[q.dtype], int(bool(causal)),
+                     _ints(q_start, "q_start"), _ints(k_start, "k_start", n_seq + 1), q.data_ptr(), k.data_ptr(),
+                     v.data_ptr(), q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ls = torch.empty((n_q, heads), dtype=torch.float32, device=q.device) if lse else None
+    _check(_lib.cf_attn_prompt(C.byref(a), dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
+                               ls.data_ptr() if lse else None, _stream()), "cf_attn_prompt")
     return (out, ls) if lse else out
 
 

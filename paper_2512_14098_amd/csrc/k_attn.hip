@@ -50,7 +50,7 @@ __device__ __forceinline__ float log_sum(float m, float l, float s2) {
 }
 
 // Most parts of one context: their weights for a tile's rows are held in LDS.
-__host__ __device__ constexpr int max_parts(int kind) { return kind ? 32 : 256; }
+__host__ __device__ constexpr int max_parts(int kind) { return kind ? 16 : 128; }
 
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -78,31 +78,31 @@ __device__ __forceinline__ int swz8(int row) {
 }
 
 // ------------------------------------------------------------------ plan
-constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-
-// Sums over the block of two numbers a thread.
-__device__ __forceinline__ void block_sum2(int64_t &x, int64_t &y, int64_t (*lds)[2]) {
+// Sums over the block of NS numbers a thread, and maxima of NM.
+template <int NT, int NS, int NM>
+__device__ __forceinline__ void block_reduce(float (&x)[NS + NM], float (*lds)[8]) {
 #pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    x += __shfl_xor(x, o);
-    y += __shfl_xor(y, o);
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) {
-    lds[threadIdx.x >> 6][0] = x;
-    lds[threadIdx.x >> 6][1] = y;
-  }
-  __syncthreads();
-  x = y = 0;
+  for (int o = 32; o; o >>= 1)
 #pragma unroll
-  for (int i = 0; i < kPlanWaves; i++) {
-    x += lds[i][0];
-    y += lds[i][1];
+    for (int i = 0; i < NS + NM; i++) {
+      const float y = __shfl_xor(x[i], o);
+      x[i] = i < NS ? x[i] + y : fmaxf(x[i], y);
+    }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int i = 0; i < NS + NM; i++) lds[threadIdx.x >> 6][i] = x[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NS + NM; i++) {
+    x[i] = lds[0][i];
+#pragma unroll
+    for (int w = 1; w < NT / 64; w++) x[i] = i < NS ? x[i] + lds[w][i] : fmaxf(x[i], lds[w][i]);
   }
 }
 
 // How the contexts of one kernel's requests are split.  n workgroups run at a time per
-// key/value head; candidate c aims at 2^c parts for each of them (c = 0, 1; c < 0: no split).  A
+// key/value head; the candidates are no split, and one and two parts for each of them.  A
 // candidate's time is estimated in keys: its parts in full rounds, or their sum over the
 // workgroups and half a part of tail, whichever is less, and `cost` keys for starting a
 // part and joining its result.
@@ -111,15 +111,18 @@ struct Split {
 };
 
 // One workgroup.  Pass 1 sums the work of either kernel, (row tiles) x (keys), and the
-// parts that each candidate length gives; pass 2 takes 1024 requests at a time, places
-// their items by a scan and writes them, a thread per item.
-__global__ __launch_bounds__(kPlanThreads) void k_attn_plan(PlanView v, const int32_t *q_start, const int32_t *kv_len,
-                                                            int n_seq, int n_tok, int G, int Hkv, int few_only,
-                                                            int big_log2, Split sp0, Split sp1) {
-  __shared__ int64_t red[kPlanWaves][2];
-  __shared__ int64_t l_at[kPlanThreads];
-  __shared__ int l_n[kPlanThreads];
-  __shared__ int l_keys[2];
+// parts that each candidate length gives; pass 2 takes NT requests at a time, places their
+// items by a scan and writes them, a thread per item.  Bound by the latency of its few
+// steps (16 to 256 requests: 5 to 6 us), so that 256 threads do better than 1024 as long as
+// one step takes all requests.
+template <int NT>
+__global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_start, const int32_t *kv_len, int n_seq,
+                                                  int n_tok, int G, int Hkv, int few_only, int big_log2, Split sp0,
+                                                  Split sp1) {
+  __shared__ float red[NT / 64][8];
+  __shared__ int64_t red64[NT / 64];
+  __shared__ int64_t l_at[NT];
+  __shared__ int l_n[NT];
   const int tid = threadIdx.x;
   auto load = [&](int i, int &tiles, int &kind, int &keys) {
     const int q0 = clampi(q_start[i], 0, n_tok), rows = max(clampi(q_start[i + 1], 0, n_tok) - q0, 0) * G;
@@ -128,56 +131,61 @@ __global__ __launch_bounds__(kPlanThreads) void k_attn_plan(PlanView v, const in
     tiles = (rows + (1 << sh) - 1) >> sh;
     keys = clampi(kv_len[i], 0, 1 << 29);  // the last part of a context has no end
   };
+  int tiles0 = 0, kind0 = 0, keys0 = 0;  // the thread's first request, kept for the later passes
+  if (tid < n_seq) load(tid, tiles0, kind0, keys0);
   // the counters of finished parts start at zero
   for (int k = 0; k < 2; k++)
-    for (int i = tid; i < v.cap_join[k] * Hkv; i += kPlanThreads) v.done[k][i] = 0;
-  if (tid < 2) l_keys[tid] = 0;
-  int tiles0 = 0, kind0 = 0, keys0 = 0;  // the thread's first request, kept for pass 2
-  if (tid < n_seq) load(tid, tiles0, kind0, keys0);
-  int64_t w[2] = {0, 0};
-  int longest[2] = {0, 0};
-  for (int i = tid; i < n_seq; i += kPlanThreads) {
+    for (int i = tid; i < v.cap_join[k] * Hkv; i += NT) v.done[k][i] = 0;
+  float w[4] = {0.f, 0.f, 0.f, 0.f};  // work of either kernel, longest contexts
+  for (int i = tid; i < n_seq; i += NT) {
     int tiles = tiles0, kind = kind0, keys = keys0;
     if (i != tid) load(i, tiles, kind, keys);
-    w[kind] += (int64_t)tiles * keys;
-    if (tiles > 0) longest[kind] = max(longest[kind], keys);
+    const float t = (float)tiles * (float)keys, ks = tiles > 0 ? (float)keys : 0.f;
+    w[0] += kind ? 0.f : t;
+    w[1] += kind ? t : 0.f;
+    w[2] = fmaxf(w[2], kind ? 0.f : ks);
+    w[3] = fmaxf(w[3], kind ? ks : 0.f);
   }
-  __syncthreads();
-  if (longest[0] > 0) atomicMax(&l_keys[0], longest[0]);
-  if (longest[1] > 0) atomicMax(&l_keys[1], longest[1]);
-  block_sum2(w[0], w[1], red);  // its barriers also cover l_keys
-  int part[2];
+  block_reduce<NT, 2, 2>(w, red);
+  // Candidate lengths: no split, and c = 0, 1: one and two parts for each workgroup.  They
+  // are above the even share by more than the sums' rounding, so the parts of split contexts
+  // number less than 2 x 2 x n.
+  int len[2][3];
+#pragma unroll
   for (int k = 0; k < 2; k++) {
     const Split sp = k ? sp1 : sp0;
-    const int keys_max = l_keys[k];
-    part[k] = 0x7fffff80;
-    if (w[k] == 0) continue;
+    const int least = max(kMinPart, (int)(w[2 + k] * 1.001f) / sp.max_parts + 2);
+#pragma unroll
+    for (int c = 0; c < 3; c++) {
+      const float even = c == 0 ? 0x1p30f : fminf(w[k] * 1.001f / (float)(sp.n * c) + 1.f, 0x1p30f);
+      len[k][c] = (max((int)even, least) + 127) & ~127;
+    }
+  }
+  float n[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int i = tid; i < n_seq; i += NT) {
+    int tiles = tiles0, kind = kind0, keys = keys0;
+    if (i != tid) load(i, tiles, kind, keys);
+#pragma unroll
+    for (int c = 0; c < 3; c++) {
+      const float t = (float)tiles * fmaxf(ceilf((float)keys / (float)(kind ? len[1][c] : len[0][c])), 1.f);
+      n[c] += kind ? 0.f : t;
+      n[3 + c] += kind ? t : 0.f;
+    }
+  }
+  block_reduce<NT, 6, 0>(n, red);
+  int part[2];
+#pragma unroll
+  for (int k = 0; k < 2; k++) {
+    const Split sp = k ? sp1 : sp0;
     float best = 0.f;
-    for (int c = -1; c < 2; c += 2) {  // no split beside one part each; two parts each
-      int len[2];
-      int64_t n[2] = {0, 0};
-      for (int e = 0; e < 2; e++) {
-        // at least the even share, so the parts of split contexts number less than 2 x 2 x n;
-        // the sum is in doubles: an estimate, then one more
-        const double even = c + e < 0 ? 0x1p30 : (double)w[k] / ((double)sp.n * (1 << min(c + e, 1))) + 1.0;
-        const int floor_len = max(kMinPart, keys_max / sp.max_parts + 1);
-        len[e] = (max((int)fmin(even, 0x1p30), floor_len) + 127) & ~127;
-      }
-      for (int i = tid; i < n_seq; i += kPlanThreads) {
-        int tiles = tiles0, kind = kind0, keys = keys0;
-        if (i != tid) load(i, tiles, kind, keys);
-        if (kind != k) continue;
-        n[0] += (int64_t)tiles * max((int)((unsigned)(keys + (unsigned)len[0] - 1u) / (unsigned)len[0]), 1);
-        n[1] += (int64_t)tiles * max((int)((unsigned)(keys + (unsigned)len[1] - 1u) / (unsigned)len[1]), 1);
-      }
-      block_sum2(n[0], n[1], red);
-      for (int e = 0; e < 2; e++) {
-        const float most = (float)min(len[e], keys_max), per = (float)n[e] / sp.n;
-        const float t = fminf(ceilf(per) * most, fmaxf((float)w[k] / sp.n, most) + 0.5f * most) + per * sp.cost;
-        if ((c < 0 && e == 0) || t < best) {
-          best = t;
-          part[k] = len[e];
-        }
+    part[k] = len[k][0];
+#pragma unroll
+    for (int c = 0; c < 3; c++) {
+      const float most = fminf((float)len[k][c], w[2 + k]), per = n[3 * k + c] / (float)sp.n;
+      const float t = fminf(ceilf(per) * most, fmaxf(w[k] / (float)sp.n, most) + 0.5f * most) + per * (float)sp.cost;
+      if (c == 0 || t < best) {
+        best = t;
+        part[k] = len[k][c];
       }
     }
   }
@@ -185,14 +193,20 @@ __global__ __launch_bounds__(kPlanThreads) void k_attn_plan(PlanView v, const in
   // the last two are bounded by the choice of the part whatever the lengths are.
   int64_t at[2] = {0, 0};
   int slots[2] = {0, 0}, joins[2] = {0, 0};
-  for (int c0 = 0; c0 < n_seq; c0 += kPlanThreads) {
-    const int i = c0 + tid, cn = min(kPlanThreads, n_seq - c0);
+  for (int c0 = 0; c0 < n_seq; c0 += NT) {
+    const int i = c0 + tid, cn = min(NT, n_seq - c0);
     int tiles = c0 ? 0 : tiles0, kind = c0 ? 0 : kind0, keys = c0 ? 0 : keys0;
     if (c0 && i < n_seq) load(i, tiles, kind, keys);
     const int parts = max((int)((unsigned)(keys + (unsigned)part[kind] - 1u) / (unsigned)part[kind]), 1);
-    for (int k = 0; k < 2; k++) {
+    // long contexts first, so that the last workgroups to start are short: three classes by
+    // the length of a part, of which a block without requests in a class skips it
+    const float most = fminf((float)part[kind], w[2 + kind]), mine_len = fminf((float)keys, (float)part[kind]);
+    const int cls = mine_len >= 0.67f * most ? 0 : mine_len >= 0.33f * most ? 1 : 2;
+    for (int kc = 0; kc < 6; kc++) {
+      const int k = kc / 3;
       if (k && few_only) break;
-      const bool mine = kind == k && tiles > 0;
+      const bool mine = kind == k && cls == kc % 3 && tiles > 0;
+      if (!__syncthreads_or(mine)) continue;
       const int64_t items = mine ? (int64_t)tiles * parts : 0;
       const int64_t x = items | (parts > 1 ? (items << 40) | ((int64_t)(mine ? tiles : 0) << 52) : 0);
       // running sums over the block
@@ -204,20 +218,20 @@ __global__ __launch_bounds__(kPlanThreads) void k_attn_plan(PlanView v, const in
         if (lane >= o) incl += y;
       }
       __syncthreads();
-      if (lane == 63) red[wv][0] = incl;
+      if (lane == 63) red64[wv] = incl;
       l_n[tid] = mine ? parts : 0;
       __syncthreads();
       int64_t before = incl - x, total = 0;
 #pragma unroll
-      for (int e = 0; e < kPlanWaves; e++) {
-        if (e < wv) before += red[e][0];
-        total += red[e][0];
+      for (int e = 0; e < NT / 64; e++) {
+        if (e < wv) before += red64[e];
+        total += red64[e];
       }
       l_at[tid] = before;
       __syncthreads();
       const int64_t low = (1ll << 40) - 1;
-      const int64_t n = total & low, room = v.cap_items[k] - at[k];
-      for (int64_t y = tid; y < min(n, room); y += kPlanThreads) {
+      const int64_t n_items = total & low, room = v.cap_items[k] - at[k];
+      for (int64_t y = tid; y < min(n_items, room); y += NT) {
         int lo = 0, hi = cn;  // the last request with items that starts at or before item y
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
@@ -233,7 +247,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attn_plan(PlanView v, const in
         }
         v.items[k][at[k] + y] = it;
       }
-      at[k] += n;
+      at[k] += n_items;
       slots[k] += (int)((uint64_t)total >> 40 & 0xfff);
       joins[k] += (int)((uint64_t)total >> 52);
     }
@@ -341,7 +355,7 @@ __device__ __forceinline__ bool read_item(const AttnArgs &a, int kind, int item,
 
 // The parts of a split context are joined by the workgroup that finishes last, in part
 // order whichever it is:  m = max m_p, l = sum l_p e^(m_p - m), o = sum o_p e^(m_p - m) / l.
-// w: LDS of this workgroup, at least max_parts x R floats and 4 per thread.
+// w: LDS of this workgroup, at least 2 x max_parts x R floats.
 template <typename T, int R>
 __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, const Item &it, int head, int row0,
                                            int n, float *w) {
@@ -361,18 +375,24 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, con
   if (!last) return;
   const float *ml = a.plan.ml[kind], *o = a.plan.o[kind];
   const int64_t base = ((int64_t)it.slot * a.Hkv + head) * R, step = (int64_t)a.Hkv * R;
-  // a row's weights of the parts; lse
+  // maxima and sums of all parts to LDS at once; then a row's weights of the parts, and lse
+  float *wl = w + it.n * R;
+  for (int x = tid; x < it.n * R; x += nt) {
+    const int p = x / R, rr = x % R;
+    if (rr >= n) continue;
+    const float2 y = load_part(ml + (base + p * step + rr) * 2);
+    w[x] = y.x;
+    wl[x] = y.y;
+  }
+  __syncthreads();
   for (int rr = tid; rr < n; rr += nt) {
     float m = kNegInf, l = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < it.n; p++) m = fmaxf(m, load_part(ml + (base + p * step + rr) * 2).x);
+    for (int p = 0; p < it.n; p++) m = fmaxf(m, w[p * R + rr]);
     const float mu = m == kNegInf ? 0.f : m;
-#pragma unroll 4
     for (int p = 0; p < it.n; p++) {
-      const float2 x = load_part(ml + (base + p * step + rr) * 2);
-      const float f = exp2_hw((x.x - mu) * a.s2);
+      const float f = exp2_hw((w[p * R + rr] - mu) * a.s2);
       w[p * R + rr] = f;
-      l = fmaf(f, x.y, l);
+      l = fmaf(f, wl[p * R + rr], l);
     }
     l_sum[rr] = l > 0.f || l != l ? 1.f / l : 0.f;
     const int j = (row0 + rr) / a.G, g = row0 + rr - j * a.G;
@@ -383,7 +403,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, con
   for (int x = tid; x < n * quads; x += nt) {
     const int rr = x / quads, d4 = x - rr * quads;
     f32x4 acc = {0, 0, 0, 0};
-#pragma unroll 8
+#pragma unroll 16
     for (int p = 0; p < it.n; p++) {
       const float *src = o + (base + p * step + rr) * a.D + d4 * 4;
       const float2 x = load_part(src), y = load_part(src + 2);
@@ -1060,7 +1080,8 @@ extern "C" cf_status cf_attn_plan(const cf_attn_desc *d, void *stream) {
   PlanView v;
   const cf_status st = check_plan(d, &v);
   if (st != CF_OK) return st;
-  k_attn_plan<<<dim3(1), dim3(kPlanThreads), 0, as_stream(stream)>>>(
+  const auto kernel = d->n_seq <= 256 ? k_attn_plan<256> : k_attn_plan<1024>;
+  kernel<<<dim3(1), dim3(d->n_seq <= 256 ? 256 : 1024), 0, as_stream(stream)>>>(
       v, d->q_start_dev, d->kv_len_dev, d->n_seq, d->n_tok, d->n_heads / d->n_kv_heads, d->n_kv_heads,
       few_only(d) ? 1 : 0, desc_groups(d) > 1 ? 8 : 7, split_of(d, 0), split_of(d, 1));
   return hip_check(hipGetLastError(), "cf_attn_plan");
