@@ -1,0 +1,145 @@
+"""Measured attention time of an LLM executor's iterations on a workload's own requests.
+
+The planner prices an iteration by a latency model: a prefill (k0 + k1 X) + k2 n for X tokens of
+n requests, a decode step d0 + d1 n (Sec. 4.1).  What such a model cannot be fitted to without a
+card is the part that depends on context lengths, the attention over the cache.  This module
+measures it: requests come from the workload's trace, an executor admits them in batches of the
+batch knob, and each iteration runs the calls that a serving step makes - cf_kv_map for the step,
+cf_kv_write and cf_attn_paged for each layer on one cf_attn_plan, cf_attn_prompt for an encoder's
+batch.  Keys, values and queries are random: only their sizes matter to the time.
+
+    python -m paper_2512_14098_amd.attn_profile --config c1 --batch 64 --layers 32
+"""
+import argparse
+
+import numpy as np
+import torch
+
+from . import cf
+from .inputs import load_config
+
+ATTRS = ("prompt", "out", "patches", "aud_in_ms", "aud_out_ms", "aud_in_tok", "aud_out_tok")
+
+
+def component_tokens(model, trace, component):
+    """Input tokens X of each request of a host trace whose type runs the component."""
+    comp = next(c for c in model["components"] if c["name"] == component)
+    runs = np.array([component in t["comps"] for t in model["types"]])
+    t = {a: np.asarray(trace[a], np.int64) for a in ATTRS if a in trace}
+    t["aud_in_tok"], t["aud_out_tok"] = -(-t["aud_in_ms"] // 80), -(-t["aud_out_ms"] // 80)
+    x = sum(t[a] for a in comp["x"])
+    keep = runs[np.asarray(trace["type"])] & (x > 0)
+    return x[keep], np.maximum(t[comp.get("n_out", "out")][keep], 1)
+
+
+class PagedExecutor:
+    """One executor's paged cache and the attention of its iterations."""
+
+    def __init__(self, slots, longest, layers, heads, kv_heads, dim, page=16, dtype=torch.bfloat16, device="cuda"):
+        self.layers, self.heads, self.kv_heads, self.dim, self.page = layers, heads, kv_heads, dim, page
+        rows = -(-longest // page)
+        n_pages = slots * rows
+        self.table = torch.full((slots, rows), -1, dtype=torch.int32, device=device)
+        self.free = torch.arange(n_pages, dtype=torch.int32, device=device)
+        self.head = torch.zeros(1, dtype=torch.int32, device=device)
+        shape = (n_pages, kv_heads, page, dim)
+        # one layer's cache serves every layer of the profile: their sizes are the same
+        self.k_cache = torch.randn(shape, dtype=dtype, device=device)
+        self.v_cache = torch.randn(shape, dtype=dtype, device=device)
+        self.qkv = torch.empty((0, heads + 2 * kv_heads, dim), dtype=dtype, device=device)
+
+    def step(self, ctx_len, new_len, n_tok, max_new):
+        """One iteration: returns its attention output (the last layer's) and the status words."""
+        if self.qkv.shape[0] < n_tok:
+            self.qkv = torch.randn((n_tok,) + tuple(self.qkv.shape[1:]), dtype=self.qkv.dtype, device=self.qkv.device)
+        x, h, g = self.qkv[:n_tok], self.heads, self.kv_heads
+        q_start, kv_len, slots, _, head, status = cf.cf_kv_map(ctx_len, new_len, self.table, self.page, self.free,
+                                                               self.head, n_tok)
+        self.head = head
+        plan = cf.cf_attn_plan(q_start, kv_len, n_tok, max_new, h, g, self.dim)
+        for _ in range(self.layers):
+            cf.cf_kv_write(x[:, h:h + g], x[:, h + g:], self.k_cache, self.v_cache, slots)
+            out = cf.cf_attn_paged(plan, x[:, :h], self.k_cache, self.v_cache, self.table)
+        return out, status
+
+
+def _timed(fn):
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    out = fn()
+    b.record()
+    b.synchronize()
+    return out, a.elapsed_time(b) * 1e-3
+
+
+def profile(config, component=None, batch=64, layers=32, heads=32, kv_heads=8, dim=128, page=16, decode_steps=4,
+            n_req=1000, seed=0, device="cuda"):
+    """Attention seconds of one prefill and of decode steps of ``batch`` requests of the
+    workload's first LLM (or ``component``), beside the latency model's seconds; for each
+    encoder, the attention of a batch of its inputs."""
+    cfg = load_config(config) if isinstance(config, str) else config
+    model = cfg["model"]
+    desc = cf.model_desc(model)
+    trace, _ = cf.cf_trace_gen(desc, [seed], n_req, device)
+    host = trace.to_numpy()
+    llm = component or next(c["name"] for c in model["components"] if c["kind"] == "LLM")
+    comp = next(c for c in model["components"] if c["name"] == llm)
+    x, out = component_tokens(model, host, llm)
+    x, out = x[:batch], out[:batch]
+    n = len(x)
+    if n == 0:
+        raise cf.CfError("no request of the trace runs " + llm)
+    ex = PagedExecutor(n, int(x.max()) + decode_steps + 1, layers, heads, kv_heads, dim, page, device=device)
+    rows = []
+    ctx = torch.zeros(n, dtype=torch.int32, device=device)
+    new = torch.as_tensor(x.astype(np.int32)).to(device)
+    ones = torch.ones(n, dtype=torch.int32, device=device)
+    k0, k1, k2 = comp["k"]
+    d0, d1 = comp.get("decode", (0.0, 0.0))
+    (_, status), _ = _timed(lambda: ex.step(ctx, new, int(x.sum()), int(x.max())))  # the first call builds buffers
+    ex.head.zero_()
+    (_, status), s = _timed(lambda: ex.step(ctx, new, int(x.sum()), int(x.max())))
+    if int(status.sum()):
+        raise cf.CfError("the cache does not hold the batch")
+    rows.append(dict(step="prefill", component=llm, requests=n, tokens=int(x.sum()), attention_s=s,
+                     model_s=k0 + k1 * float(x.sum()) + k2 * n))
+    ctx = new.clone()
+    for i in range(decode_steps):
+        (_, status), s = _timed(lambda: ex.step(ctx, ones, n, 1))
+        ctx = ctx + ones
+        rows.append(dict(step="decode %d" % i, component=llm, requests=n, tokens=int(x.sum()) + n * (i + 1),
+                         attention_s=s, model_s=d0 + d1 * n))
+    for c in model["components"]:
+        if c["kind"] != "ENC":
+            continue
+        e, _ = component_tokens(model, host, c["name"])
+        if any(v.endswith("_ms") for v in c["x"]):
+            e = -(-e // 20)  # audio frames of 20 ms
+        e = np.minimum(e[:batch], 4096)  # a window of long inputs
+        if len(e) == 0:
+            continue
+        starts = torch.as_tensor(np.concatenate([[0], np.cumsum(e)]).astype(np.int32)).to(device)
+        y = torch.randn((int(e.sum()), 3 * 16, 64), dtype=torch.bfloat16, device=device)
+        run = lambda: [cf.cf_attn_prompt(y[:, :16], y[:, 16:32], y[:, 32:], starts, causal=False)
+                       for _ in range(layers)]
+        _timed(run)
+        _, s = _timed(run)
+        rows.append(dict(step="encode", component=c["name"], requests=len(e), tokens=int(e.sum()), attention_s=s,
+                         model_s=c["k"][0] + c["k"][1] * float(e.sum()) + c["k"][2] * len(e)))
+    return rows
+
+
+def main(argv=None):
+    p = argparse.ArgumentParser(description="attention time of an LLM executor's iterations on this GPU")
+    p.add_argument("--config", default="c1")
+    p.add_argument("--component")
+    for name, value in (("batch", 64), ("layers", 32), ("heads", 32), ("kv-heads", 8), ("dim", 128), ("page", 16)):
+        p.add_argument("--" + name, type=int, default=value)
+    a = p.parse_args(argv)
+    for r in profile(a.config, a.component, a.batch, a.layers, a.heads, a.kv_heads, a.dim, a.page):
+        print("%-10s %-8s %4d requests %8d tokens  attention %9.3f ms  latency model %9.3f ms"
+              % (r["step"], r["component"], r["requests"], r["tokens"], r["attention_s"] * 1e3, r["model_s"] * 1e3))
+
+
+if __name__ == "__main__":
+    main()
