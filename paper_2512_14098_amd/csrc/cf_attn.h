@@ -84,7 +84,8 @@ struct PlanHdr {
 struct PlanItem {
   int32_t seq, tile, part, n;  // part of n of the context of a tile of rows
   int32_t slot, join;          // n > 1: the tile's first partial result, its counter
-  int32_t pad[2];
+  int32_t q0, nq, nk;          // the request's first token, new tokens and keys
+  int32_t pad[3];
 };
 struct PlanView {
   PlanHdr *hdr;
@@ -106,7 +107,7 @@ struct Rows {
 struct AttnArgs {
   const void *q, *k, *v;
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;  // elements
-  const int32_t *q_start, *kv;  // kv: cached lengths (paged) or key starts (packed)
+  const int32_t *q_start, *kv;  // packed sequences: query and key starts
   const int32_t *table;
   int32_t max_pages, n_pages, page_log2;
   int32_t n_seq, n_tok, n_k, H, Hkv, G, D, causal;
@@ -117,20 +118,5 @@ struct AttnArgs {
 };
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
-
-template <bool PAGED>
-__device__ __forceinline__ Rows rows_of(const AttnArgs &a, int seq, int &k0) {
-  Rows r;
-  r.q0 = clampi(a.q_start[seq], 0, a.n_tok);
-  r.nq = max(clampi(a.q_start[seq + 1], 0, a.n_tok) - r.q0, 0);
-  if (PAGED) {
-    k0 = 0;
-    r.nk = (int)min((int64_t)max(a.kv[seq], 0), (int64_t)a.max_pages << a.page_log2);
-  } else {
-    k0 = clampi(a.kv[seq], 0, a.n_k);
-    r.nk = max(clampi(a.kv[seq + 1], 0, a.n_k) - k0, 0);
-  }
-  return r;
-}
 
 }  // namespace cf

@@ -122,7 +122,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
   __shared__ float red[NT / 64][8];
   __shared__ int64_t red64[NT / 64];
   __shared__ int64_t l_at[NT];
-  __shared__ int l_n[NT];
+  __shared__ int l_n[NT], l_first[NT];
   const int tid = threadIdx.x;
   auto load = [&](int i, int &tiles, int &kind, int &keys) {
     const int q0 = clampi(q_start[i], 0, n_tok), rows = max(clampi(q_start[i + 1], 0, n_tok) - q0, 0) * G;
@@ -198,17 +198,26 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
     int tiles = c0 ? 0 : tiles0, kind = c0 ? 0 : kind0, keys = c0 ? 0 : keys0;
     if (c0 && i < n_seq) load(i, tiles, kind, keys);
     const int parts = max((int)((unsigned)(keys + (unsigned)part[kind] - 1u) / (unsigned)part[kind]), 1);
-    // long contexts first, so that the last workgroups to start are short: three classes by
-    // the length of a part, of which a block without requests in a class skips it
-    const float most = fminf((float)part[kind], w[2 + kind]), mine_len = fminf((float)keys, (float)part[kind]);
-    const int cls = mine_len >= 0.67f * most ? 0 : mine_len >= 0.33f * most ? 1 : 2;
+    // Long parts first, so that the last workgroups to start are short: three classes by the
+    // length of a part.  A many-row tile t from the last sees keys - t R / G of the keys: its
+    // request's tiles fall into the classes one after the other.
+    const float most = fminf((float)part[kind], w[2 + kind]);
+    int from[4] = {0, 0, 0, tiles};
+#pragma unroll
+    for (int c = 1; c < 3; c++) {
+      const float least = (c == 1 ? 0.67f : 0.33f) * most;  // of the classes before c
+      const float extra = fminf((float)keys, (float)keys - least);
+      const bool all = kind == 0 || parts > 1;
+      const int in = extra < 0.f ? 0 : all ? tiles : (int)fminf(extra * (float)G / (float)(1 << big_log2) + 1.f, 0x1p24f);
+      from[c] = clampi(in, from[c - 1], tiles);
+    }
     for (int kc = 0; kc < 6; kc++) {
-      const int k = kc / 3;
+      const int k = kc / 3, first = from[kc % 3], count = from[kc % 3 + 1] - first;
       if (k && few_only) break;
-      const bool mine = kind == k && cls == kc % 3 && tiles > 0;
+      const bool mine = kind == k && count > 0;
       if (!__syncthreads_or(mine)) continue;
-      const int64_t items = mine ? (int64_t)tiles * parts : 0;
-      const int64_t x = items | (parts > 1 ? (items << 40) | ((int64_t)(mine ? tiles : 0) << 52) : 0);
+      const int64_t items = mine ? (int64_t)count * parts : 0;
+      const int64_t x = items | (parts > 1 ? (items << 40) | ((int64_t)(mine ? count : 0) << 52) : 0);
       // running sums over the block
       const int lane = tid & 63, wv = tid >> 6;
       int64_t incl = x;
@@ -220,6 +229,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
       __syncthreads();
       if (lane == 63) red64[wv] = incl;
       l_n[tid] = mine ? parts : 0;
+      l_first[tid] = first;
       __syncthreads();
       int64_t before = incl - x, total = 0;
 #pragma unroll
@@ -239,8 +249,10 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
         }
         const int64_t b = l_at[lo];
         const unsigned np = (unsigned)max(l_n[lo], 1), rest = (unsigned)(y - (b & low));
-        const int tile = (int)(rest / np), pi = (int)(rest - tile * np);
-        PlanItem it = {c0 + lo, tile, pi, (int)np, -1, -1, {0, 0}};
+        const int tile = (int)(rest / np), pi = (int)(rest - tile * np), seq = c0 + lo;
+        const int q0 = clampi(q_start[seq], 0, n_tok);
+        PlanItem it = {seq, l_first[lo] + tile, pi, (int)np, -1, -1, q0,
+                       max(clampi(q_start[seq + 1], 0, n_tok) - q0, 0), max(kv_len[seq], 0), {0, 0, 0}};
         if (np > 1) {
           it.slot = slots[k] + (int)((uint64_t)b >> 40 & 0xfff) + tile * (int)np;
           it.join = joins[k] + (int)((uint64_t)b >> 52) + tile;
@@ -337,11 +349,14 @@ struct Item {
 };
 
 // Item `item` of the plan, if there is one and it names what exists.
-__device__ __forceinline__ bool read_item(const AttnArgs &a, int kind, int item, Item &it) {
+__device__ __forceinline__ bool read_item(const AttnArgs &a, int kind, int item, Item &it, Rows &r) {
   if (item >= min(a.plan.hdr->n_items[kind], a.plan.cap_items[kind])) return false;
   const PlanItem p = a.plan.items[kind][item];
   const int len = a.plan.hdr->part[kind];
   it = Item{p.seq, p.tile, p.part, p.n, p.slot, p.join, 0, 0x7fffffff};
+  r.q0 = clampi(p.q0, 0, a.n_tok);
+  r.nq = clampi(p.nq, 0, a.n_tok - r.q0);
+  r.nk = (int)min((int64_t)max(p.nk, 0), (int64_t)a.max_pages << a.page_log2);
   if ((unsigned)p.seq >= (unsigned)a.n_seq || p.tile < 0 || p.n < 1) return false;
   if (p.n > 1) {
     if (p.part < 0 || p.part >= p.n || p.slot < 0 || p.slot > a.plan.cap_slots[kind] - p.n ||
@@ -434,9 +449,8 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = (int)(blockIdx.x % (unsigned)a.Hkv), item = (int)(blockIdx.x / (unsigned)a.Hkv);
   Item it;
-  if (!read_item(a, 0, item, it)) return;
-  int k0;
-  const Rows r = rows_of<true>(a, it.seq, k0);
+  Rows r;
+  if (!read_item(a, 0, item, it, r)) return;
   const int n_rows = r.nq * a.G, row0 = it.tile * kRowsSmall;
   if (row0 >= n_rows) return;
   const int row = row0 + (lane & 15), j = min(row, n_rows - 1) / a.G, g = min(row, n_rows - 1) - j * a.G;
@@ -653,28 +667,36 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   Rows r;
   int k0 = 0;
   if (PAGED) {
-    if (!read_item(a, 1, item, it)) return;
-    r = rows_of<true>(a, it.seq, k0);
+    if (!read_item(a, 1, item, it, r)) return;
   } else {
     // sequence i owns the tiles from floor(first row / R) + i on; 64 probes at a time, the
-    // last round of them over neighbours
-    int lo = 0, n = a.n_seq, q = 0;
+    // last round of them over neighbours, which also gives the sequence's bounds
+    int lo = 0, n = a.n_seq, q, q1, e0, e1;
     for (;;) {
-      const int step = (n + 63) >> 6;
-      q = clampi(a.q_start[lo + min(lane * step, n - 1)], 0, a.n_tok);
-      const bool le = lane * step < n && (int)((unsigned)(q * a.G) / R) + lo + lane * step <= item;
-      const int cnt = __builtin_popcountll(__ballot(le)), at = max(cnt - 1, 0);
+      const int step = (n + 63) >> 6, i = lo + min(lane * step, n - 1);
+      q = clampi(a.q_start[i], 0, a.n_tok);
+      q1 = clampi(a.q_start[i + 1], 0, a.n_tok);
+      e0 = clampi(a.kv[i], 0, a.n_k);
+      e1 = clampi(a.kv[i + 1], 0, a.n_k);
+      const bool le = lane * step < n && (int)((unsigned)(q * a.G) / R) + i <= item;
+      const int at = max(__builtin_popcountll(__ballot(le)) - 1, 0);
       q = __builtin_amdgcn_readlane(q, at);
+      q1 = __builtin_amdgcn_readlane(q1, at);
+      e0 = __builtin_amdgcn_readlane(e0, at);
+      e1 = __builtin_amdgcn_readlane(e1, at);
       lo += at * step;
       if (step == 1) break;
       n = min(step, n - at * step);
     }
     it.seq = lo;
     it.tile = item - ((int)((unsigned)(q * a.G) / R) + lo);
+    r.q0 = q;
+    r.nq = max(q1 - q, 0);
+    k0 = e0;
+    r.nk = max(e1 - e0, 0);
     it.lo = 0;
     it.end = 0x7fffffff;
     it.n = 1;
-    r = rows_of<false>(a, lo, k0);
   }
   const int n_rows = __builtin_amdgcn_readfirstlane(r.nq * a.G);  // below 2^31, as all row numbers
   const int n_rt = (n_rows + R - 1) / R;
@@ -721,7 +743,7 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   i32x4 kr[NL], vr[NL];
 #pragma unroll
   for (int i = 0; i < NL; i++) kr[i] = vr[i] = i32x4{0, 0, 0, 0};
-  int ids = 0;
+  uint64_t k_at = 0, v_at = 0;
   bool bad = false;
 
   // Loads of a tile's keys or values; edge: some may not be there or the tile be past the
@@ -729,13 +751,22 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   const int lrow = tid / CH, lcol = tid % CH;
   const bool col_ok = lcol * 8 < a.D;
   const int to_load = min(r.nk, it.lo + 64 * n_tiles);
-  auto load_ids = [&](int n) CF_INLINE {  // page ids of tiles n .. n + 7 (n a multiple of 8), one lane per 16 keys
-    const int key = it.lo + 64 * n + 16 * (lane & 31);
-    if ((lane >> 5) == ((n >> 3) & 1)) ids = key < hi ? trow[key >> a.page_log2] : -1;
+  // Where the keys and values of tiles n .. n + 7 begin (n a multiple of 8), a lane for each 16
+  // keys, the lanes of 16 tiles in two halves: looked up once for all waves' loads, since the
+  // address arithmetic of a page at every load would outweigh the exponentials.
+  auto load_ids = [&](int n) CF_INLINE {
+    if ((lane >> 5) == ((n >> 3) & 1)) {
+      const int key = it.lo + 64 * n + 16 * (lane & 31);
+      const int id = key < hi ? trow[key >> a.page_log2] : -1;
+      const int64_t at = (int64_t)id * page_elems + (int64_t)(key & page_mask) * a.D;
+      const bool in = (unsigned)id < (unsigned)a.n_pages;
+      k_at = (uint64_t)(in ? kc + at : (const T *)g_zeros);
+      v_at = (uint64_t)(in ? vc + at : (const T *)g_zeros);
+    }
   };
   // packed: the lane's row of the next tile to load
   const T *kp = kc + (int64_t)lrow * a.k_tok + lcol * 8, *vp = vc + (int64_t)lrow * a.v_tok + lcol * 8;
-  auto load = [&](i32x4 (&x)[NL], const T *src, const T *&at, int64_t tok, int n, auto edge) CF_INLINE {
+  auto load = [&](i32x4 (&x)[NL], uint64_t where, const T *&at, int64_t tok, int n, auto edge) CF_INLINE {
     const int t0 = it.lo + 64 * n;
     if (!col_ok) return;
 #pragma unroll
@@ -743,11 +774,10 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
       const int rr = i * RS + lrow;
       const T *p;
       if (PAGED) {
-        const int kg = __builtin_amdgcn_readfirstlane(rr >> 4);
-        const int id = __builtin_amdgcn_readlane(ids, ((n & 15) << 2) + kg);
-        const bool in = (unsigned)id < (unsigned)a.n_pages;
-        const int64_t base = (in ? id : 0) * page_elems + (int64_t)((t0 + 16 * kg) & page_mask) * a.D;
-        p = (in ? src + base : (const T *)g_zeros) + (unsigned)((rr & 15) * a.D + lcol * 8);
+        const int l16 = ((n & 15) << 2) + __builtin_amdgcn_readfirstlane(rr >> 4);
+        const uint32_t alo = __builtin_amdgcn_readlane((uint32_t)where, l16);
+        const uint32_t ahi = __builtin_amdgcn_readlane((uint32_t)(where >> 32), l16);
+        p = (const T *)((uint64_t)ahi << 32 | alo) + (unsigned)((rr & 15) * a.D + lcol * 8);
       } else {
         p = at + i * RS * tok;
       }
@@ -765,9 +795,9 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   };
   // keys nk and values nk - 1 to registers, or from there to LDS
   auto fetch = [&](int nk, auto edge) CF_INLINE {
-    if (PAGED && (nk & 7) == 0) load_ids(nk);
-    load(kr, kc, kp, a.k_tok, nk, edge);
-    load(vr, vc, vp, a.v_tok, nk - 1, edge);
+    load(kr, k_at, kp, a.k_tok, nk, edge);
+    load(vr, v_at, vp, a.v_tok, nk - 1, edge);
+    if (PAGED && (nk & 7) == 0) load_ids(nk + 8);  // in place of tiles before nk
   };
   auto put = [&](int nk, T *kd, T *vd, auto edge) CF_INLINE {
     store(kr, kd);
@@ -874,12 +904,15 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
 #pragma unroll
   for (int k = 0; k < 4; k++) pf[k] = __builtin_bit_cast(V8, i32x4{0, 0, 0, 0});
   store(vr, lds_v[1]);
-  if (PAGED) load_ids(0);
+  if (PAGED) {
+    load_ids(0);
+    load_ids(8);
+  }
   {
     i32x4 first[NL];
 #pragma unroll
     for (int i = 0; i < NL; i++) first[i] = i32x4{0, 0, 0, 0};
-    load(first, kc, kp, a.k_tok, 0, Int<1>());
+    load(first, k_at, kp, a.k_tok, 0, Int<1>());
     fetch(1, Int<1>());
     store(first, lds_k[0]);
   }
@@ -1106,7 +1139,7 @@ extern "C" cf_status cf_attn_paged(const cf_attn_desc *d, const cf_kv_cache *cac
     return set_error(CF_EINVAL, "queries or output are not 16-byte aligned");
   a.q = q_dev; a.k = cache->k_dev; a.v = cache->v_dev;
   a.q_tok = q_tok; a.q_head = q_head;
-  a.q_start = d->q_start_dev; a.kv = d->kv_len_dev; a.table = table_dev;
+  a.table = table_dev;
   a.max_pages = max_pages; a.n_pages = cache->n_pages; a.page_log2 = log2_of(cache->page);
   a.n_seq = d->n_seq; a.n_tok = d->n_tok;
   a.H = d->n_heads; a.Hkv = d->n_kv_heads; a.G = a.H / a.Hkv; a.D = d->head_dim; a.causal = 1;
