@@ -122,7 +122,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
   __shared__ float red[NT / 64][8];
   __shared__ int64_t red64[NT / 64];
   __shared__ int64_t l_at[NT];
-  __shared__ int l_n[NT], l_first[NT];
+  __shared__ int l_n[NT];
   const int tid = threadIdx.x;
   auto load = [&](int i, int &tiles, int &kind, int &keys) {
     const int q0 = clampi(q_start[i], 0, n_tok), rows = max(clampi(q_start[i + 1], 0, n_tok) - q0, 0) * G;
@@ -199,25 +199,16 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
     if (c0 && i < n_seq) load(i, tiles, kind, keys);
     const int parts = max((int)((unsigned)(keys + (unsigned)part[kind] - 1u) / (unsigned)part[kind]), 1);
     // Long parts first, so that the last workgroups to start are short: three classes by the
-    // length of a part.  A many-row tile t from the last sees keys - t R / G of the keys: its
-    // request's tiles fall into the classes one after the other.
-    const float most = fminf((float)part[kind], w[2 + kind]);
-    int from[4] = {0, 0, 0, tiles};
-#pragma unroll
-    for (int c = 1; c < 3; c++) {
-      const float least = (c == 1 ? 0.67f : 0.33f) * most;  // of the classes before c
-      const float extra = fminf((float)keys, (float)keys - least);
-      const bool all = kind == 0 || parts > 1;
-      const int in = extra < 0.f ? 0 : all ? tiles : (int)fminf(extra * (float)G / (float)(1 << big_log2) + 1.f, 0x1p24f);
-      from[c] = clampi(in, from[c - 1], tiles);
-    }
-    for (int kc = 0; kc < 6; kc++) {
-      const int k = kc / 3, first = from[kc % 3], count = from[kc % 3 + 1] - first;
-      if (k && few_only) break;
-      const bool mine = kind == k && count > 0;
+    // length of a part (256 decodes of 300 to 4300 keys: 436 us against 468).  Not for the
+    // many-row kernel, whose neighbouring tiles of one request share keys in the L2.
+    const float most = fminf((float)part[0], w[2]), mine_len = fminf((float)keys, (float)part[0]);
+    const int cls = kind ? 3 : mine_len >= 0.67f * most ? 0 : mine_len >= 0.33f * most ? 1 : 2;
+    for (int kc = 0; kc < 4; kc++) {
+      const int k = kc / 3;
+      const bool mine = cls == kc && tiles > 0;
       if (!__syncthreads_or(mine)) continue;
-      const int64_t items = mine ? (int64_t)count * parts : 0;
-      const int64_t x = items | (parts > 1 ? (items << 40) | ((int64_t)(mine ? count : 0) << 52) : 0);
+      const int64_t items = mine ? (int64_t)tiles * parts : 0;
+      const int64_t x = items | (parts > 1 ? (items << 40) | ((int64_t)(mine ? tiles : 0) << 52) : 0);
       // running sums over the block
       const int lane = tid & 63, wv = tid >> 6;
       int64_t incl = x;
@@ -229,7 +220,6 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
       __syncthreads();
       if (lane == 63) red64[wv] = incl;
       l_n[tid] = mine ? parts : 0;
-      l_first[tid] = first;
       __syncthreads();
       int64_t before = incl - x, total = 0;
 #pragma unroll
@@ -251,7 +241,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
         const unsigned np = (unsigned)max(l_n[lo], 1), rest = (unsigned)(y - (b & low));
         const int tile = (int)(rest / np), pi = (int)(rest - tile * np), seq = c0 + lo;
         const int q0 = clampi(q_start[seq], 0, n_tok);
-        PlanItem it = {seq, l_first[lo] + tile, pi, (int)np, -1, -1, q0,
+        PlanItem it = {seq, tile, pi, (int)np, -1, -1, q0,
                        max(clampi(q_start[seq + 1], 0, n_tok) - q0, 0), max(kv_len[seq], 0), {0, 0, 0}};
         if (np > 1) {
           it.slot = slots[k] + (int)((uint64_t)b >> 40 & 0xfff) + tile * (int)np;
@@ -752,14 +742,19 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   const bool col_ok = lcol * 8 < a.D;
   const int to_load = min(r.nk, it.lo + 64 * n_tiles);
   // Where the keys and values of tiles n .. n + 7 begin (n a multiple of 8), a lane for each 16
-  // keys, the lanes of 16 tiles in two halves: looked up once for all waves' loads, since the
-  // address arithmetic of a page at every load would outweigh the exponentials.
+  // keys, the lanes of 16 tiles in two halves.  The page ids are loaded 12 tiles ahead and made
+  // addresses 8 ahead of the next half's first use: a round neither waits for an id nor does
+  // the arithmetic of a page at every load.
+  int ids = -1;
   auto load_ids = [&](int n) CF_INLINE {
+    const int key = it.lo + 64 * n + 16 * (lane & 31);
+    ids = key < hi ? trow[key >> a.page_log2] : -1;
+  };
+  auto place = [&](int n) CF_INLINE {
     if ((lane >> 5) == ((n >> 3) & 1)) {
       const int key = it.lo + 64 * n + 16 * (lane & 31);
-      const int id = key < hi ? trow[key >> a.page_log2] : -1;
-      const int64_t at = (int64_t)id * page_elems + (int64_t)(key & page_mask) * a.D;
-      const bool in = (unsigned)id < (unsigned)a.n_pages;
+      const int64_t at = (int64_t)ids * page_elems + (int64_t)(key & page_mask) * a.D;
+      const bool in = (unsigned)ids < (unsigned)a.n_pages;
       k_at = (uint64_t)(in ? kc + at : (const T *)g_zeros);
       v_at = (uint64_t)(in ? vc + at : (const T *)g_zeros);
     }
@@ -797,7 +792,8 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   auto fetch = [&](int nk, auto edge) CF_INLINE {
     load(kr, k_at, kp, a.k_tok, nk, edge);
     load(vr, v_at, vp, a.v_tok, nk - 1, edge);
-    if (PAGED && (nk & 7) == 0) load_ids(nk + 8);  // in place of tiles before nk
+    if (PAGED && (nk & 7) == 4) place(nk + 4);  // in place of tiles nk - 12 .. nk - 5
+    if (PAGED && (nk & 7) == 0) load_ids(nk + 8);
   };
   auto put = [&](int nk, T *kd, T *vd, auto edge) CF_INLINE {
     store(kr, kd);
@@ -906,6 +902,7 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   store(vr, lds_v[1]);
   if (PAGED) {
     load_ids(0);
+    place(0);
     load_ids(8);
   }
   {
