@@ -3,7 +3,8 @@
  * statistical plan evaluation of Cornfigurator (arXiv 2512.14098):
  * request traces, flow-based screening (Sec. 4.3, Alg. 2 phase 1),
  * request-level simulation (Alg. 2 phase 3) and goodput selection
- * (Sec. 3.2, Sec. 6.1).
+ * (Sec. 3.2, Sec. 6.1); and the attention of an LLM executor's iterations
+ * over a paged cache, to measure what its latency model stands for.
  *
  * Conventions
  *  - Pointers named *_dev are device pointers (HIP global memory), owned and
@@ -567,12 +568,12 @@ cf_status cf_kv_write(const cf_kv_cache *cache, int32_t n_tok, const void *k_dev
 
 /* One step's attention: n_tok new tokens of n_seq requests (starts
  * q_start_dev, cached lengths with the new tokens kv_len_dev, as cf_kv_map
- * writes them), n_heads query heads, query head h reading key/value head
+ * writes them; read by cf_attn_plan only), n_heads query heads, query head h reading key/value head
  * h / (n_heads / n_kv_heads).  max_new bounds a request's new tokens as far
  * as the caller knows (n_tok if it does not); it picks kernels, not results.
  * work_dev: cf_attn_plan_bytes(...) bytes, 16-byte aligned, the caller's; it
  * holds the plan and the partial results of split contexts, so calls that
- * share it must not overlap. */
+ * share it must not overlap, from whichever stream. */
 typedef struct cf_attn_desc {
   int32_t n_seq, n_tok, max_new;
   int32_t n_heads, n_kv_heads, head_dim;

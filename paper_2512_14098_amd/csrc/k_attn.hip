@@ -113,7 +113,7 @@ struct Split {
 // One workgroup.  Pass 1 sums the work of either kernel, (row tiles) x (keys), and the
 // parts that each candidate length gives; pass 2 takes NT requests at a time, places their
 // items by a scan and writes them, a thread per item.  Bound by the latency of its few
-// steps (16 to 256 requests: 5 to 6 us), so that 256 threads do better than 1024 as long as
+// steps (16 to 256 requests: 6 us; with 64-bit divisions and a scan for each count 17), so that 256 threads do better than 1024 as long as
 // one step takes all requests.
 template <int NT>
 __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_start, const int32_t *kv_len, int n_seq,
@@ -429,6 +429,13 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, con
 // O^T = V^T P^T, whose first operand is read transposed from the wave's own
 // copy of the tile in LDS.  The next tile's keys and values are loaded while
 // one is worked on.  The waves' results are joined at the end.
+//
+// Bound by memory: 256 requests of 1771 keys on average (32 heads on 8, 128
+// columns, bf16, pages of 16) 318 us, 5.8 TB/s of cache, where a kernel that only
+// reads reaches 6.3; one request of 32767 keys on 32 key/value heads 94 us, 5.7
+// TB/s.  Two workgroups a CU hold 128 KB in flight; a third (168 registers, 7
+// spilled) is 10 % slower.  The matrix unit is busy 4 % of the time, also where
+// one of its 16 rows is used.
 template <typename T, int KS, int DB, int DS>
 __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) {
   using V8 = typename Elem<T>::v8;
@@ -645,6 +652,19 @@ __device__ __forceinline__ void matrix_order() {
 // share of keys n + 1 + g and values n + g, loaded one round earlier: those go to
 // the LDS halves of keys n - 1 + g and values n - 2 + g, which both groups have
 // read by then, and are complete when group 0 begins its matrix phase n + 1 + g.
+// With one group a workgroup runs on its own, two or three of them a CU, and needs
+// one barrier a round.
+//
+// Bound by the matrix unit and its power: one causal sequence of 32767 tokens (32
+// heads on 8, 128 columns, bf16) 7.19 ms, 1.22 PFLOP/s, as a large library matrix
+// product on the same card; the unit is busy 68 % of the cycles at 1.65 GHz.  What
+// the steps to it were worth on that case: a tile's work in one stream, operands
+// read right before their use, 9.6 ms; the maximum allowed to lag 8.7; two groups
+// out of step 9.5 and, with the operand reads ordered ahead, 8.1; the exponentials
+// kept in the vector phase 7.3.  Short sequences pay 8 to 10 us a workgroup to
+// start and end: 16 causal prompts of 1387 tokens on average 447 us, 0.79 PFLOP/s.
+// With 64 columns the exponentials take longer than the products: 16 full images
+// of 623 patches, 16 heads, 52 us, 0.54 PFLOP/s.
 template <typename T, int KS, int DB, int DS, int NG, bool PAGED>
 __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_attn_many(AttnArgs a) {
   using V8 = typename Elem<T>::v8;

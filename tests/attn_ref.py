@@ -61,9 +61,9 @@ def attend(q, k, v, sees, scale, kind):
             s = min(max(int(sees[j]), 0), m)
             if s == 0:
                 continue
-            x = (kh[:s] * q[j, h].astype(np.float64)[None]) * scale
-            e = np.abs(x).sum(1).max() * (D + 4) * 2.0 ** -24
-            x = x.sum(1)
+            qj = q[j, h].astype(np.float64) * scale
+            e = (np.abs(kh[:s]) @ np.abs(qj)).max() * (D + 4) * 2.0 ** -24
+            x = kh[:s] @ qj
             top = x.max()
             p = np.exp(x - top)
             l = p.sum()

@@ -467,3 +467,85 @@ def test_scores_of_any_size(cf):
     k[50], k[150], q[10:20] = k[50] * 30, k[150] * 60, 0
     _compare(*cf.cf_attn_prompt(q, k, v, _i32([0, n]), causal=False, scale=2.0, lse=True),
              _want_prompt(q, k, v, [n], [n], False, 2.0, "bf16"))
+
+
+# ------------------------------------------------------------------ enough rows for two wave groups
+def _sampled(q, k, v, rows, sees, heads, scale, kind):
+    """Reference of some rows and heads: q [n][H][D] of one sequence (device tensors)."""
+    G = q.shape[1] // k.shape[1]
+    out = []
+    for h in heads:
+        out.append(attn_ref.attend(q[rows][:, h:h + 1].float().cpu().numpy(),
+                                   k[:, h // G:h // G + 1].float().cpu().numpy(),
+                                   v[:, h // G:h // G + 1].float().cpu().numpy(), [sees[r] for r in rows], scale, kind))
+    return [np.concatenate(p, axis=1) for p in zip(*out)]
+
+
+@pytest.mark.parametrize("kind,dim", [("bf16", 128), ("fp16", 96), ("fp16", 128), ("bf16", 72)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompt_of_many_rows(cf, kind, dim, causal):
+    """3100 rows of each of 16 key/value heads, keys fewer, as many and more than the queries."""
+    n, H = 3100, 16
+    for m in (2900, n, 3333):
+        _say("many rows", kind, dim, causal, m)
+        g = torch.Generator(device="cuda").manual_seed(m)
+        q = torch.randn((n, H, dim), generator=g, device="cuda").to(DT[kind])
+        k, v = (torch.randn((m, H, dim), generator=g, device="cuda").to(DT[kind]) for _ in range(2))
+        sees = [min(max(m - n + j + 1, 0), m) if causal else m for j in range(n)]
+        rows = sorted({0, 1, 63, 64, 127, 128, 199, 200, 201, 255, 256, 300, 511, 1600, 2815, 2816, 3071, 3080, n - 2, n - 1})
+        out, lse = cf.cf_attn_prompt(q, k, v, _i32([0, n]), _i32([0, m]), causal=causal, lse=True)
+        heads = [0, 7, 15]
+        _compare(out[rows][:, heads], lse[rows][:, heads], _sampled(q, k, v, rows, sees, heads, dim ** -0.5, kind))
+
+
+@pytest.mark.parametrize("kind,ctx,new,heads,kv_heads,dim,page", [
+    ("bf16", 150, 3100, 16, 16, 128, 16), ("fp16", 1, 3100, 32, 16, 96, 64), ("bf16", 40000, 3100, 16, 4, 128, 16)])
+def test_paged_many_rows(cf, kind, ctx, new, heads, kv_heads, dim, page):
+    """The same over a cache, the last one with its context split; NaN in the unused pages and,
+    in one value past most rows' sight, an infinity."""
+    _say("paged many rows", kind, ctx, new)
+    kv = ctx + new
+    g = torch.Generator(device="cuda").manual_seed(new)
+    used = -(-kv // page)
+    perm = torch.randperm(used + 9, generator=g, device="cuda")
+    table = perm[:used].int()[None].contiguous()
+    k, v = (torch.randn((kv, kv_heads, dim), generator=g, device="cuda").to(DT[kind]) for _ in range(2))
+    q = torch.randn((new, heads, dim), generator=g, device="cuda").to(DT[kind])
+    special = kv - 40
+    v[special, 1, 3] = float("inf")
+    kc, vc = (torch.full((used + 9, kv_heads, page, dim), float("nan"), device="cuda").to(DT[kind]) for _ in range(2))
+    at = torch.arange(kv, device="cuda")
+    slots = perm[at // page] * page + at % page
+    cf.cf_kv_write(k, v, kc, vc, slots)
+    plan = cf.cf_attn_plan(_i32([0, new]), _i32([kv]), new, new, heads, kv_heads, dim)
+    out, lse = cf.cf_attn_paged(plan, q, kc, vc, table, lse=True)
+    again = cf.cf_attn_paged(plan, q, kc, vc, table)
+    assert torch.equal(out, again)
+    rows = [0, 1, 31, 64, 255, 256, 1000, 2047, 2048, 3000, new - 42, new - 41]
+    G = heads // kv_heads
+    hs = [0, G, heads - 1]
+    v[special, 1, 3] = 0
+    _compare(out[rows][:, hs], lse[rows][:, hs],
+             _sampled(q, k, v, rows, [ctx + j + 1 for j in range(new)], hs, dim ** -0.5, kind))
+    seen = out[new - 40:, G:2 * G]
+    assert bool(torch.isinf(seen[:, :, 3]).all()) and bool(torch.isfinite(out[:new - 40]).all())
+    rest = torch.ones(dim, dtype=torch.bool, device="cuda")
+    rest[3] = False
+    assert bool(torch.isfinite(seen[:, :, rest]).all())
+
+
+def test_plan_of_many_requests(cf):
+    """More requests than one pass of the plan takes, with and without new tokens, few and many
+    rows, split and whole contexts, in one step."""
+    rng = np.random.default_rng(11)
+    n = 1500
+    new = np.where(rng.random(n) < 0.3, 0, 1)
+    new[[5, 700, 1400]] = [40, 90, 17]
+    kv = np.where(new > 0, rng.integers(1, 60, n) + new, rng.integers(0, 60, n))
+    kv[[6, 1200]] = 9000
+    new[[6, 1200]] = 1
+    ctx = (kv - new).tolist()
+    c = _paged_case("bf16", ctx, new.tolist(), 2, 1, 64, 16)
+    want = _want_paged(c, ctx, new.tolist(), 0.125, "bf16")
+    for max_new in (None, 1):
+        _compare(*_run_paged(cf, c, new.tolist(), 2, 1, 64, max_new=max_new), want)
