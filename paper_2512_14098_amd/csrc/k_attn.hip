@@ -727,14 +727,6 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   const int all = min(causal ? off + __builtin_amdgcn_readlane(j, 0) + 1 : r.nk, hi);
   const int h = lane >> 5;
 
-  V8 qf[KS];
-  const T *qp = (const T *)a.q + (int64_t)(r.q0 + j) * a.q_tok + (int64_t)(head * a.G + g) * a.q_head;
-#pragma unroll
-  for (int ks = 0; ks < KS; ks++) {
-    const int c = ks * 2 + h;
-    qf[ks] = __builtin_bit_cast(V8, load16(c * 8 < a.D ? (const void *)(qp + c * 8) : (const void *)g_zeros));
-  }
-
   const int64_t page_elems = (int64_t)a.Hkv * a.D << a.page_log2;
   const int64_t head_off = (int64_t)head * a.D << a.page_log2;
   const T *kc = (const T *)a.k + (PAGED ? head_off : (int64_t)k0 * a.k_tok + head * a.k_head);
@@ -743,6 +735,7 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   const int32_t *trow = PAGED ? a.table + (int64_t)it.seq * a.max_pages : nullptr;
   const int n_tiles = hi > it.lo ? (hi - it.lo + 63) >> 6 : 0;
 
+  V8 qf[KS];
   f32x16 o[DB], s[2];
 #pragma unroll
   for (int d = 0; d < DB; d++)
@@ -898,7 +891,7 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   };
 
   // One round: the matrix phase of tile n, then its vector phase.  edge: some row may not see
-  // all the keys of a tile that the round touches, or a tile not be there.
+  // all its keys or all the values it stores, or a fetched tile not be there.
   auto round = [&](int n, auto buf, auto edge) CF_INLINE {
     const int B = buf.value;
     __builtin_amdgcn_s_setprio(1);
@@ -931,6 +924,13 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
     for (int i = 0; i < NL; i++) first[i] = i32x4{0, 0, 0, 0};
     load(first, k_at, kp, a.k_tok, 0, Int<1>());
     fetch(1, Int<1>());
+    // the queries after the first keys and values: those are waited for first
+    const T *qp = (const T *)a.q + (int64_t)(r.q0 + j) * a.q_tok + (int64_t)(head * a.G + g) * a.q_head;
+#pragma unroll
+    for (int ks = 0; ks < KS; ks++) {
+      const int c = ks * 2 + h;
+      qf[ks] = __builtin_bit_cast(V8, load16(c * 8 < a.D ? (const void *)(qp + c * 8) : (const void *)g_zeros));
+    }
     store(first, lds_k[0]);
   }
   __syncthreads();
@@ -939,9 +939,9 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
     fetch(2, Int<1>());
     __syncthreads();
   }
-  // rounds whose tiles, up to the ones they fetch, every row of the workgroup sees; two at a
-  // time, one per LDS buffer
-  const int n_main = (min(all_wg, hi) - it.lo) / 64 - 1 - NG;
+  // rounds whose tile every row of the workgroup sees, as it does the values that they store,
+  // and whose fetched keys are there; two at a time, one per LDS buffer
+  const int n_main = min((min(all_wg, hi) - it.lo) / 64 + 1 - NG, (r.nk - it.lo) / 64 - 1 - NG);
   int n = 0;
   for (; n + 2 <= n_main; n += 2) {
     round(n, Int<0>(), Int<0>());
@@ -973,13 +973,23 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   } else if (row < n_rows) {
     const int64_t orow = (int64_t)(r.q0 + j) * a.H + head * a.G + g;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+    // Of two neighbouring groups of 8 columns, each of which lies half in this lane and half in
+    // the one 32 away, either lane takes one whole: 16-byte stores.
 #pragma unroll
     for (int d = 0; d < DB; d++)
 #pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const int e = d * 32 + 8 * q + 4 * h;
-        const f32x4 x = {o[d][4 * q] * inv, o[d][4 * q + 1] * inv, o[d][4 * q + 2] * inv, o[d][4 * q + 3] * inv};
-        if (e < a.D) *(V4 *)((T *)a.out + orow * a.D + e) = __builtin_convertvector(x, V4);
+      for (int q = 0; q < 4; q += 2) {
+        uint2 x[2];
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const int i = 4 * (q + e);
+          const f32x4 y = {o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+          x[e] = __builtin_bit_cast(uint2, __builtin_convertvector(y, V4));
+        }
+        const auto lo = __builtin_amdgcn_permlane32_swap(x[0].x, x[1].x, false, false);
+        const auto hi2 = __builtin_amdgcn_permlane32_swap(x[0].y, x[1].y, false, false);
+        const int e = d * 32 + 8 * (q + h);
+        if (e < a.D) *(uint4 *)((T *)a.out + orow * a.D + e) = make_uint4(lo[0], hi2[0], lo[1], hi2[1]);
       }
     if (a.lse && h == 0) a.lse[orow] = log_sum(m, l, a.s2);
   }
