@@ -513,9 +513,9 @@ cf_status cf_goodput_curve(const cf_fine_out *fine, int32_t n_plans, int32_t K, 
 cf_status cf_select_best(const double *goodput_dev, int32_t n, int32_t *best_dev, void *stream);
 
 /* ------------------------------------------------------------------ attention over a paged cache
- * The attention of an LLM executor's iteration (prefill and decode steps,
- * Sec. 2) and the page bookkeeping it reads: what a profile of an executor
- * (Sec. 5.1) measures where an iteration's time depends on request lengths.
+ * The attention of an LLM executor's iteration (a prefill or a decode step)
+ * and the page bookkeeping it reads: what a profile of an executor (Sec. 5.1)
+ * measures where an iteration's time depends on request lengths.
  *
  * Cache: keys and values of one layer, each [n_pages][n_kv_heads][page]
  * [head_dim] of 16-bit elements; page is a power of two, 16..256.  Slot s is
@@ -538,8 +538,7 @@ typedef struct cf_kv_cache {
   int32_t dtype; /* CF_BF16 / CF_F16, also of queries, keys, values and outputs */
 } cf_kv_cache;
 
-/* Block tables and slot maps of one step from request lengths (the batches an
- * LLM executor forms, Sec. 2).  Request i has ctx_len_dev[i] cached tokens and
+/* Block tables and slot maps of one step from request lengths.  Request i has ctx_len_dev[i] cached tokens and
  * new_len_dev[i] new ones, packed in request order; its new pages are the next
  * ceil((ctx+new)/page) - ceil(ctx/page) entries of free_dev [n_free] from
  * *head_dev on, in request order, entered in its row of table_dev
@@ -599,8 +598,9 @@ cf_status cf_attn_plan(const cf_attn_desc *d, void *stream);
  * i, sees keys 0 .. kv_len - new + j: out = sum_k p_k v_k / sum_k p_k,
  * p_k = exp(scale q.k).  A row that sees no key (kv_len 0, or fewer keys than
  * new tokens) gives 0, and lse -inf.  Keys past kv_len are never used, whatever
- * they hold; pages outside the cache read as zeros.  q_dev [n_tok][n_heads]
- * [head_dim] with strides q_tok and q_head; out_dev packed; lse_dev
+ * they hold; pages outside the cache read as zeros.  Rows of tokens that no
+ * request owns are left as they were.  q_dev [n_tok][n_heads][head_dim] with
+ * strides q_tok and q_head; out_dev packed; lse_dev
  * [n_tok][n_heads] float, log of the sum of the p_k, or NULL.  Sums, the
  * softmax's maximum and sum, and outputs are kept in 32 bits; the p_k are
  * rounded to the element type for their product with the values.

@@ -1,9 +1,9 @@
 """Measured attention time of an LLM executor's iterations on a workload's own requests.
 
 The planner prices an iteration by a latency model: a prefill (k0 + k1 X) + k2 n for X tokens of
-n requests, a decode step d0 + d1 n (Sec. 4.1).  What such a model cannot be fitted to without a
-card is the part that depends on context lengths, the attention over the cache.  This module
-measures it: requests come from the workload's trace, an executor admits them in batches of the
+n requests, a decode step d0 + d1 n.  What such a model cannot be fitted to without a
+card is the part that depends on context lengths, the attention over the cache, one share of what
+an executor's profile (Sec. 5.1) holds.  This module measures it: requests come from the workload's trace, an executor admits them in batches of the
 batch knob, and each iteration runs the calls that a serving step makes - cf_kv_map for the step,
 cf_kv_write and cf_attn_paged for each layer on one cf_attn_plan, cf_attn_prompt for an encoder's
 batch.  Keys, values and queries are random: only their sizes matter to the time.

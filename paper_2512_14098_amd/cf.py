@@ -699,9 +699,9 @@ def cf_kv_map(ctx_len, new_len, table, page, free_pages, head, n_tok):
         raise CfError("table: expected int32 [%d][max_pages]" % n)
     if n_tok < 0:
         raise CfError("n_tok %d" % n_tok)
-    # the 32-bit results are parts of one allocation
-    q_start, kv_len, pos, head_out, status = torch.empty(
-        3 * n + n_tok + 2, dtype=torch.int32, device=ctx_len.device).split((n + 1, n, n_tok, 1, n))
+    # the 32-bit results are parts of one allocation (untracked ones: views cost as much as the launch)
+    q_start, kv_len, pos, head_out, status = torch.unsafe_split_with_sizes(
+        torch.empty(3 * n + n_tok + 2, dtype=torch.int32, device=ctx_len.device), (n + 1, n, n_tok, 1, n))
     slots = torch.empty(n_tok, dtype=torch.int64, device=ctx_len.device)
     base = q_start.data_ptr()
     _check(_lib.cf_kv_map(n, _ints(ctx_len, "ctx_len"), _ints(new_len, "new_len", n), page, _ints(table, "table"),
@@ -766,7 +766,7 @@ def cf_attn_paged(plan, q, k_cache, v_cache, table, scale=None, lse=False):
         raise CfError("q: expected %d tokens, got %d" % (d.n_tok, q.shape[0]))
     if table.dim() != 2 or table.shape[0] != d.n_seq:
         raise CfError("table: expected [%d][max_pages]" % d.n_seq)
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
     ls = torch.empty((d.n_tok, d.n_heads), dtype=torch.float32, device=q.device) if lse else None
     _check(_lib.cf_attn_paged(C.byref(d), C.byref(c), _ints(table, "table"), table.shape[1], q.data_ptr(), q.stride(0),
                               q.stride(1), d.head_dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
@@ -790,7 +790,7 @@ def cf_attn_prompt(q, k, v, q_start, k_start=None, causal=True, scale=None, lse=
     a = cf_attn_seqs(n_seq, n_q, n_k, heads, kv_heads, dim, ATTN_DTYPE[q.dtype], int(bool(causal)),
                      _ints(q_start, "q_start"), _ints(k_start, "k_start", n_seq + 1), q.data_ptr(), k.data_ptr(),
                      v.data_ptr(), q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1))
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
     ls = torch.empty((n_q, heads), dtype=torch.float32, device=q.device) if lse else None
     _check(_lib.cf_attn_prompt(C.byref(a), dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
                                ls.data_ptr() if lse else None, _stream()), "cf_attn_prompt")

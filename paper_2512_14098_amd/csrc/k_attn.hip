@@ -438,12 +438,12 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, con
 // copy of the tile in LDS.  The next tile's keys and values are loaded while
 // one is worked on.  The waves' results are joined at the end.
 //
-// Bound by memory: 256 requests of 1771 keys on average (32 heads on 8, 128
-// columns, bf16, pages of 16) 318 us, 5.8 TB/s of cache, where a kernel that only
-// reads reaches 6.3; one request of 32767 keys on 32 key/value heads 94 us, 5.7
-// TB/s.  Two workgroups a CU hold 128 KB in flight; a third (168 registers, 7
-// spilled) is 10 % slower.  The matrix unit is busy 4 % of the time, also where
-// one of its 16 rows is used.
+// Bound by memory: 256 requests of 1767 keys on average (32 heads on 8, 128
+// columns, bf16, pages of 16) 287 us, 6.5 TB/s of cache (a kernel that only reads
+// reaches 6.3 with ordinary loads); one request of 32767 keys on 32 key/value heads
+// 85 us, 6.3 TB/s.  Two workgroups a CU hold 128 KB in flight; a third (168
+// registers, 7 spilled) is 10 % slower.  The matrix unit is busy 4 % of the time,
+// also where one of its 16 rows is used.
 template <typename T, int KS, int DB, int DS>
 __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) {
   using V8 = typename Elem<T>::v8;
@@ -664,15 +664,15 @@ __device__ __forceinline__ void matrix_order() {
 // one barrier a round.
 //
 // Bound by the matrix unit and its power: one causal sequence of 32767 tokens (32
-// heads on 8, 128 columns, bf16) 7.19 ms, 1.22 PFLOP/s, as a large library matrix
-// product on the same card; the unit is busy 68 % of the cycles at 1.65 GHz.  What
+// heads on 8, 128 columns, bf16) 7.16 ms, 1.23 PFLOP/s, as a large library matrix
+// product on the same card; the unit is busy 70 % of the cycles at 1.65 GHz.  What
 // the steps to it were worth on that case: a tile's work in one stream, operands
 // read right before their use, 9.6 ms; the maximum allowed to lag 8.7; two groups
 // out of step 9.5 and, with the operand reads ordered ahead, 8.1; the exponentials
-// kept in the vector phase 7.3.  Short sequences pay 8 to 10 us a workgroup to
-// start and end: 16 causal prompts of 1387 tokens on average 447 us, 0.79 PFLOP/s.
-// With 64 columns the exponentials take longer than the products: 16 full images
-// of 623 patches, 16 heads, 52 us, 0.54 PFLOP/s.
+// kept in the vector phase 7.3.  Short sequences pay 8 us a workgroup to start and
+// end: 16 causal prompts of 1387 tokens on average 408 us, 0.87 PFLOP/s.  With 64
+// columns the exponentials take longer than the products: 16 full images of 623
+// patches, 16 heads, 53 us, 0.54 PFLOP/s.
 template <typename T, int KS, int DB, int DS, int NG, bool PAGED>
 __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_attn_many(AttnArgs a) {
   using V8 = typename Elem<T>::v8;

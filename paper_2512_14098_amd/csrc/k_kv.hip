@@ -45,8 +45,8 @@ __device__ __forceinline__ int64_t scan_before(int64_t x, int64_t *wave_sum, int
 // request's first token known, the pages it needs.  The requests that own some
 // of the workgroup's tokens go to a list in LDS, and each token finds its own
 // there by bisection.  A new page's first token enters the page in the table.
-// Bound by the latency of its loads and scans: 64 requests 3.6 us, 256 whole prompts
-// (428,070 tokens) 9.4 us.
+// Bound by the latency of its loads and scans: 64 requests 3.3 us, 256 whole prompts
+// (428,070 tokens) 9.5 us.
 __global__ __launch_bounds__(kMapThreads) void k_kv_map(MapArgs a) {
   __shared__ int64_t wave_sum[kMapThreads / 64];
   __shared__ int32_t l_req[kMapTokens], l_first[kMapTokens], l_page[kMapTokens];
@@ -163,7 +163,7 @@ struct WriteArgs {
 // One thread per 16-byte piece of the keys (blockIdx.y 0) or values (1): a copy,
 // bound by memory.  Tokens of a page are neighbours in their head's block, so a
 // prompt's rows are written in whole lines: 52,808 tokens of 8 x 128 in 74 us, 5.8
-// TB/s read and written; 256 tokens 2.7 us.
+// TB/s read and written; 256 tokens 2.8 us.
 __global__ __launch_bounds__(256) void k_kv_write(WriteArgs a) {
   const bool is_v = blockIdx.y != 0;
   const uint4 *src = is_v ? a.v : a.k;
