@@ -130,17 +130,22 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
   __shared__ float red[NT / 64][8];
   __shared__ int64_t red64[NT / 64];
   __shared__ int64_t l_at[NT];
-  __shared__ int l_n[NT];
+  __shared__ int l_n[NT], l_rows[NT][3];
   const int tid = threadIdx.x;
+  int q0 = 0, nq = 0, nk = 0;  // of the request loaded last
   auto load = [&](int i, int &tiles, int &kind, int &keys) {
-    const int q0 = clampi(q_start[i], 0, n_tok), rows = max(clampi(q_start[i + 1], 0, n_tok) - q0, 0) * G;
+    q0 = clampi(q_start[i], 0, n_tok);
+    nq = max(clampi(q_start[i + 1], 0, n_tok) - q0, 0);
+    nk = max(kv_len[i], 0);
+    const int rows = nq * G;
     kind = (!few_only && rows > kRowsSmall) ? 1 : 0;
     const int sh = kind ? big_log2 : 4;
     tiles = (rows + (1 << sh) - 1) >> sh;
-    keys = clampi(kv_len[i], 0, 1 << 29);  // the last part of a context has no end
+    keys = min(nk, 1 << 29);  // the last part of a context has no end
   };
   int tiles0 = 0, kind0 = 0, keys0 = 0;  // the thread's first request, kept for the later passes
   if (tid < n_seq) load(tid, tiles0, kind0, keys0);
+  const int first_q0 = q0, first_nq = nq, first_nk = nk;
   // the counters of finished parts start at zero
   for (int k = 0; k < 2; k++)
     for (int i = tid; i < v.cap_join[k] * Hkv; i += NT) v.done[k][i] = 0;
@@ -204,7 +209,14 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
   for (int c0 = 0; c0 < n_seq; c0 += NT) {
     const int i = c0 + tid, cn = min(NT, n_seq - c0);
     int tiles = c0 ? 0 : tiles0, kind = c0 ? 0 : kind0, keys = c0 ? 0 : keys0;
+    q0 = first_q0;
+    nq = first_nq;
+    nk = first_nk;
     if (c0 && i < n_seq) load(i, tiles, kind, keys);
+    __syncthreads();  // the items of the requests before have been written
+    l_rows[tid][0] = q0;
+    l_rows[tid][1] = nq;
+    l_rows[tid][2] = nk;
     const int parts = max((int)((unsigned)(keys + (unsigned)part[kind] - 1u) / (unsigned)part[kind]), 1);
     // Long parts first, so that the last workgroups to start are short: three classes by the
     // length of a part (256 decodes of 300 to 4300 keys: 436 us against 468).  Not for the
@@ -247,10 +259,8 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
         }
         const int64_t b = l_at[lo];
         const unsigned np = (unsigned)max(l_n[lo], 1), rest = (unsigned)(y - (b & low));
-        const int tile = (int)(rest / np), pi = (int)(rest - tile * np), seq = c0 + lo;
-        const int q0 = clampi(q_start[seq], 0, n_tok);
-        PlanItem it = {seq, tile, pi, (int)np, -1, -1, q0,
-                       max(clampi(q_start[seq + 1], 0, n_tok) - q0, 0), max(kv_len[seq], 0), {0, 0, 0}};
+        const int tile = (int)(rest / np), pi = (int)(rest - tile * np);
+        PlanItem it = {c0 + lo, tile, pi, (int)np, -1, -1, l_rows[lo][0], l_rows[lo][1], l_rows[lo][2], {0, 0, 0}};
         if (np > 1) {
           it.slot = slots[k] + (int)((uint64_t)b >> 40 & 0xfff) + tile * (int)np;
           it.join = joins[k] + (int)((uint64_t)b >> 52) + tile;
