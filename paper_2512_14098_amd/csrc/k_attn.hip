@@ -1050,9 +1050,12 @@ bool few_only(const cf_attn_desc *d) {
 // sequence of 16384, 16 heads of 128: 1880 us against 2130), one where the work is in short
 // ones (4 x 1024, 32 heads: 64 us against 78) or too little for one workgroup of 256 rows a
 // CU (1 x 1024, 32 heads on 8: 29 us against 35); with 64 columns the exponentials outweigh
-// the products and one group is always faster, with 256 two do not fit the registers.
-int groups_of(int D, int64_t rows, int n_seq, int Hkv) {
-  return D > 64 && D <= 128 && rows >= 2048ll * n_seq && rows * Hkv >= 192 * 256 ? 2 : 1;
+// the products and one group is always faster, with 256 two do not fit the registers.  The
+// work counts as long where the mean sequence is, or a longest one that makes a quarter of
+// all rows (chunks of 2048 among 100 decodes: 314 us with two groups, 341 with one).
+int groups_of(int D, int64_t rows, int64_t longest, int n_seq, int Hkv) {
+  const bool is_long = rows >= 2048ll * n_seq || (longest >= 4096 && 4 * longest >= rows);
+  return D > 64 && D <= 128 && is_long && rows * Hkv >= 192 * 256 ? 2 : 1;
 }
 
 template <typename T, bool PAGED>
@@ -1084,7 +1087,9 @@ bool scale_ok(float s) { return s > 0.f && s <= 1e38f; }
 }  // namespace
 
 static int desc_groups(const cf_attn_desc *d) {
-  return groups_of(d->head_dim, (int64_t)d->n_tok * (d->n_heads / d->n_kv_heads), d->n_seq, d->n_kv_heads);
+  const int64_t G = d->n_heads / d->n_kv_heads;
+  return groups_of(d->head_dim, d->n_tok * G, (d->max_new < d->n_tok ? d->max_new : d->n_tok) * G, d->n_seq,
+                   d->n_kv_heads);
 }
 
 // Workgroups of the kernels that run at a time per key/value head, as the plan counts on
@@ -1206,7 +1211,7 @@ extern "C" cf_status cf_attn_prompt(const cf_attn_seqs *p, float scale, void *ou
   if (p->dtype != CF_BF16 && p->dtype != CF_F16) return set_error(CF_EINVAL, "dtype %d", p->dtype);
   if (!scale_ok(scale)) return set_error(CF_EINVAL, "scale %g is not finite and > 0", (double)scale);
   const int64_t G = p->n_heads / p->n_kv_heads;
-  const int groups = groups_of(p->head_dim, p->n_q * G, p->n_seq, p->n_kv_heads);
+  const int groups = groups_of(p->head_dim, p->n_q * G, 0, p->n_seq, p->n_kv_heads);
   const int64_t blocks = ((int64_t)p->n_q * G / (kRowsGroup * groups) + p->n_seq) * p->n_kv_heads;
   if ((int64_t)p->n_q * p->n_heads > 0x7fffffffll || blocks >= (1ll << 24))
     return set_error(CF_EINVAL, "n_q x n_heads or n_seq x n_kv_heads too large");

@@ -549,3 +549,40 @@ def test_plan_of_many_requests(cf):
     want = _want_paged(c, ctx, new.tolist(), 0.125, "bf16")
     for max_new in (None, 1):
         _compare(*_run_paged(cf, c, new.tolist(), 2, 1, 64, max_new=max_new), want)
+
+
+@pytest.mark.parametrize("max_new", [3100, 8])
+def test_long_chunk_among_decodes(cf, max_new):
+    """A chunk of 3100 tokens with running and waiting requests around it: the many-row kernel with
+    two groups and the few-row kernel in one step, and with a bound on new tokens that is too low."""
+    ctx, new, heads, kv_heads, dim, page = [70, 33, 20, 500, 8], [1, 3100, 0, 1, 3], 32, 16, 128, 32
+    n = len(ctx)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    kv = [c + m for c, m in zip(ctx, new)]
+    pages = [-(-x // page) for x in kv]
+    perm = torch.randperm(sum(pages) + 3, generator=g, device="cuda")
+    table = torch.full((n, max(pages)), -1, dtype=torch.int32, device="cuda")
+    kc, vc = (torch.full((sum(pages) + 3, kv_heads, page, dim), float("nan"), device="cuda").to(torch.bfloat16)
+              for _ in range(2))
+    ks, vs, at = [], [], 0
+    for i in range(n):
+        table[i, :pages[i]] = perm[at:at + pages[i]].int()
+        k, v = (torch.randn((kv[i], kv_heads, dim), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+        t = torch.arange(kv[i], device="cuda")
+        cf.cf_kv_write(k, v, kc, vc, perm[at + t // page] * page + t % page)
+        ks.append(k)
+        vs.append(v)
+        at += pages[i]
+    q = torch.randn((sum(new), heads, dim), generator=g, device="cuda").to(torch.bfloat16)
+    starts = np.concatenate([[0], np.cumsum(new)])
+    plan = cf.cf_attn_plan(_i32(starts), _i32(kv), sum(new), max_new, heads, kv_heads, dim)
+    out, lse = cf.cf_attn_paged(plan, q, kc, vc, table, lse=True)
+    hs = [0, 3, 31]
+    for i in range(n):
+        rows = [r for r in (0, 1, 2, 7, 127, 128, 1000, 2559, 2560, 3098, 3099) if r < new[i]]
+        if not rows:
+            continue
+        o = int(starts[i])
+        want = _sampled(q[o:o + new[i]], ks[i], vs[i], rows, [ctx[i] + j + 1 for j in range(new[i])], hs, dim ** -0.5,
+                        "bf16")
+        _compare(out[o:o + new[i]][rows][:, hs], lse[o:o + new[i]][rows][:, hs], want)
