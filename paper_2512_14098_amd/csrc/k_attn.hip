@@ -13,9 +13,9 @@
 //
 // A key that a row does not see has p_k = 0, but 0 times an infinity or a NaN
 // in its value would still reach the row.  Values past a sequence's keys are
-// loaded as zeros; in a tile that only some of a workgroup's rows see, such
-// values are zeroed on their way to LDS, and at the end, if there were any,
-// added to the rows that see them (which makes those outputs infinite or NaN).
+// loaded as zeros; in a tile with a key that some or all of a workgroup's rows
+// do not see, such values are zeroed on their way to LDS, and at the end, if there
+// were any, added to the rows that see them (which makes those outputs infinite or NaN).
 #include "cf_attn.h"
 
 namespace cf {
@@ -311,7 +311,7 @@ __device__ __forceinline__ bool special(T x) {
   return (__builtin_bit_cast(uint16_t, x) & kExpMask<T>) == kExpMask<T>;
 }
 
-// The infinities and NaN among the values of keys [from, to), which only some
+// The infinities and NaN among the values of keys [from, to), which not all
 // of the rows row0 .. row0 + n - 1 see, added to the results just written.
 template <typename T, bool PAGED>
 __device__ __forceinline__ void add_specials(const AttnArgs &a, const Rows &r, int k0, int seq, int slot, int R,
@@ -537,7 +537,7 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
   if (w < n_tiles) load(0);
   for (int n = 0; w + 4 * n < n_tiles; n++) {
     const int t0 = it.lo + 32 * (w + 4 * n);
-    if (t0 + 32 > all && seen > all) {
+    if (t0 + 32 > all && r.nk > all) {  // also where no row sees them
 #pragma unroll
       for (int i = 0; i < NV; i++) bad |= take_specials<T>(vr[i]);
     }
@@ -828,7 +828,7 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   };
   auto put = [&](int nk, T *kd, T *vd, auto edge) CF_INLINE {
     store(kr, kd);
-    if (edge.value && it.lo + 64 * nk > all_wg && seen > all_wg) {
+    if (edge.value && it.lo + 64 * nk > all_wg && r.nk > all_wg) {  // also where no row sees them
       asm volatile("");  // a branch: not worth computing for every tile
 #pragma unroll
       for (int i = 0; i < NL; i++) bad |= take_specials<T>(vr[i]);
