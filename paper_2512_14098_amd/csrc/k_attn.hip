@@ -8,8 +8,10 @@
 // with a larger maximum m' first scales l and o by exp(m - m').  Exponentials
 // are taken in base 2, log2(e) folded into the scale.  Scores, m, l and o are
 // fp32; the p_k of a tile are rounded to the element type as the matrix
-// instruction's operand (relative error at most 2^-8 in bf16, 2^-11 in fp16,
-// as the output's own rounding).
+// instruction's operand, by the output's own rounding: relative error at most
+// 2^-8 in bf16; in fp16 2^-11, and for weights below its normal range (2^-29 of
+// the largest with few rows, 2^-21 with many) an absolute one of 2^-40 and 2^-32 of the
+// largest.  l sums the p_k before that rounding.
 //
 // A key that a row does not see has p_k = 0, but 0 times an infinity or a NaN
 // in its value would still reach the row.  Values past a sequence's keys are
@@ -44,9 +46,18 @@ __device__ __forceinline__ float2 load_part(const float *p) {
 }
 __device__ __forceinline__ void parts_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// Weights p_k, and so l and o, are held 2^shift times too large in fp16, whose normal range
+// ends at 2^-14: unscaled, weights below 2^-25 of the largest would be lost to o, but not to
+// l.  The few-row kernel's largest weight is 1, the many-row kernel's at most 2^8, so the scaled
+// ones stay at or below 2^15.  The factor cancels in o / l and costs an addition a tile.
+template <typename T>
+constexpr float weight_shift(int kind) {
+  return __is_same(T, __bf16) ? 0.f : kind ? 7.f : 15.f;
+}
+
 // Log of the sum of exponentials from the running maximum and sum, natural.
-__device__ __forceinline__ float log_sum(float m, float l, float s2) {
-  return l == 0.f ? kNegInf : (m * s2 + __log2f(l)) * 0.69314718055994531f;
+__device__ __forceinline__ float log_sum(float m, float l, float s2, float shift) {
+  return l == 0.f ? kNegInf : (m * s2 + (__log2f(l) - shift)) * 0.69314718055994531f;
 }
 
 // Most parts of one context: their weights for a tile's rows are held in LDS.
@@ -419,7 +430,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, con
     }
     l_sum[rr] = l > 0.f || l != l ? 1.f / l : 0.f;
     const int j = (row0 + rr) / a.G, g = row0 + rr - j * a.G;
-    if (a.lse) a.lse[(int64_t)(r.q0 + j) * a.H + head * a.G + g] = log_sum(m, l, a.s2);
+    if (a.lse) a.lse[(int64_t)(r.q0 + j) * a.H + head * a.G + g] = log_sum(m, l, a.s2, weight_shift<T>(kind));
   }
   __syncthreads();
   const int quads = a.D / 4;
@@ -565,6 +576,7 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
       }
     mx = max_halves(max_rows16(mx));
     const float mn = fmaxf(m, mx), mu = mn == kNegInf ? 0.f : mn * a.s2;
+    const float mp = mu - weight_shift<T>(0);
     const float alpha = exp2_hw(fmaf(m, a.s2, -mu));
     m = mn;
     V8 pf;
@@ -573,7 +585,7 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
     for (int b = 0; b < 2; b++)
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        const float p = exp2_hw(fmaf(s[b][i], a.s2, -mu));
+        const float p = exp2_hw(fmaf(s[b][i], a.s2, -mp));
         ps += p;
         pf[b * 4 + i] = (T)p;
       }
@@ -625,7 +637,7 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
       const int64_t orow = (int64_t)(r.q0 + jj) * a.H + head * a.G + gg;
       const float inv = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
       *(V4 *)((T *)a.out + orow * a.D + d4 * 4) = __builtin_convertvector(oo * inv, V4);
-      if (a.lse && d4 == 0) a.lse[orow] = log_sum(mm, ll, a.s2);
+      if (a.lse && d4 == 0) a.lse[orow] = log_sum(mm, ll, a.s2, weight_shift<T>(0));
     }
   }
   if (any_bad)
@@ -890,12 +902,12 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
 #pragma unroll
       for (int d = 0; d < DB; d++) o[d] = o[d] * alpha;
     }
-    const float mu = m == kNegInf ? 0.f : m * a.s2;
+    const float mp = m == kNegInf ? 0.f : m * a.s2 - weight_shift<T>(1);
 #pragma unroll
     for (int b = 0; b < 2; b++)
 #pragma unroll
       for (int i = 0; i < 16; i++) {
-        const float p = exp2_hw(fmaf(s[b][i], a.s2, -mu));
+        const float p = exp2_hw(fmaf(s[b][i], a.s2, -mp));
         l += p;
         pf[b * 2 + (i >> 3)][i & 7] = (T)p;
       }
@@ -1009,7 +1021,7 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
         const int e = d * 32 + 8 * (q + h);
         if (e < a.D) *(uint4 *)((T *)a.out + orow * a.D + e) = make_uint4(lo[0], hi2[0], lo[1], hi2[1]);
       }
-    if (a.lse && h == 0) a.lse[orow] = log_sum(m, l, a.s2);
+    if (a.lse && h == 0) a.lse[orow] = log_sum(m, l, a.s2, weight_shift<T>(1));
   }
   if (any_bad)
     add_specials<T, PAGED>(a, r, k0, it.seq, it.n > 1 ? it.slot + it.part : -1, R, head, row0, min(n_rows - row0, R),

@@ -1,4 +1,4 @@
-"""Edges of the paged-cache calls against plain 64-bit forms: what rows must not see."""
+"""Edges of the paged-cache calls against plain 64-bit forms: what rows must not see, small weights."""
 import numpy as np
 import pytest
 
@@ -85,3 +85,60 @@ def test_last_value_is_hidden_from_256_heads(cf, paged):
     else:
         out = cf.cf_attn_prompt(q, k, v, _i32([0, n]))
     _only_last_row(out[:, hs], want, n, 7)
+
+
+# ------------------------------------------------------------------ small weights in fp16
+def _tail(n_q, heads, m, dim, seed):
+    """One key with the score 17.5 and value 0 before m - 1 keys with the score 0: weights of
+    e^-17.5 = 2.5e-8 of the largest, below half of fp16's least number, whose sum is 8e-4."""
+    rng = np.random.default_rng(seed)
+    q = np.zeros((n_q, heads, dim), np.float32)
+    k = np.zeros((m, 1, dim), np.float32)
+    q[:, :, 0], k[0, 0, 0] = 1.0, 17.5
+    v = rng.uniform(0.5, 1.5, (m, 1, dim)).astype(np.float32)
+    v[0] = 0
+    return [torch.from_numpy(x).half().cuda() for x in (q, k, v)]
+
+
+def _check_tail(got, q, k, v, sees):
+    """As attn_ref's bound, its term for weights below the normal range smaller by the 2^7 by which
+    weights are scaled at least (the largest is then 2^7 or more): 2^-32 of the largest a key."""
+    pick = [0, len(sees) - 1]
+    for j in pick:
+        s = sees[j]
+        x = k[:s, 0].double().cpu().numpy() @ q[j, 0].double().cpu().numpy()
+        p = np.exp(x - x.max())
+        vv = v[:s, 0].double().cpu().numpy()
+        l = p.sum()
+        out, A = p @ vv / l, p @ np.abs(vv) / l
+        e = 17.5 * (q.shape[2] + 4) * 2.0 ** -24
+        tol = (2 * 2.0 ** -11 + 2 * (2 * e + 2.0 ** -20) + (s + 64) * 2.0 ** -23) * A + 2.0 ** -32 * np.abs(vv).sum(0) / l + 2.0 ** -24
+        err = np.abs(got[0][j].double().cpu().numpy() - out[None])
+        assert (err <= tol[None]).all(), (j, float(err.max()), float(tol.min()), float(out.max()))
+        lse = x.max() + np.log(l)
+        assert abs(float(got[1][j, 0]) - lse) <= 2 * e + (s + 64) * 2.0 ** -23 + lse * 2.0 ** -22 + 2.0 ** -20
+
+
+@pytest.mark.parametrize("n_q,heads,dim", [(1, 4, 64), (1, 16, 128), (3, 16, 64), (140, 2, 128), (9, 16, 256)])
+def test_many_small_weights_of_a_cache(cf, n_q, heads, dim):
+    """Few and many rows, the context split and whole (a second request fills the plan)."""
+    m, page = 32766, 64
+    _say("tail", n_q, heads, dim)
+    q, k, v = _tail(n_q, heads, m, dim, n_q)
+    n_pages = -(-m // page)
+    kc, vc = (torch.zeros((n_pages, 1, page, dim), dtype=torch.float16, device="cuda") for _ in range(2))
+    cf.cf_kv_write(k, v, kc, vc, torch.arange(m, device="cuda"))
+    row = torch.arange(n_pages, dtype=torch.int32, device="cuda")
+    for n in (1, 600):
+        starts = _i32(np.arange(n + 1) * n_q)
+        plan = cf.cf_attn_plan(starts, _i32([m] * n), n * n_q, n_q, heads, 1, dim)
+        got = cf.cf_attn_paged(plan, q.repeat(n, 1, 1), kc, vc, row.repeat(n, 1), scale=1.0, lse=True)
+        _check_tail([x[-n_q:] for x in got], q, k, v, [m - n_q + j + 1 for j in range(n_q)])
+
+
+@pytest.mark.parametrize("n_q,heads,dim", [(1, 2, 64), (300, 2, 128), (3100, 16, 96)])
+def test_many_small_weights_of_a_prompt(cf, n_q, heads, dim):
+    m = 32766
+    q, k, v = _tail(n_q, heads, m, dim, n_q)
+    got = cf.cf_attn_prompt(q, k, v, _i32([0, n_q]), _i32([0, m]), causal=False, scale=1.0, lse=True)
+    _check_tail(got, q, k, v, [m] * n_q)
