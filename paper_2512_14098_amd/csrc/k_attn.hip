@@ -1045,7 +1045,7 @@ cf_status check_desc(const cf_attn_desc *d) {
     return set_error(CF_EINVAL, "n_seq %d, n_tok %d, max_new %d", d->n_seq, d->n_tok, d->max_new);
   const cf_status st = check_heads(d->n_heads, d->n_kv_heads, d->head_dim);
   if (st != CF_OK) return st;
-  // row numbers are 32-bit and a grid has at most 2^24 - 1 workgroups of 256 threads
+  // row numbers are 32-bit and a grid has fewer than 2^24 workgroups of 256 threads
   if ((int64_t)d->n_tok * d->n_heads > 0x7fffffffll ||
       ((int64_t)d->n_tok * d->n_heads / d->n_kv_heads / kRowsSmall + d->n_seq + 4096) * d->n_kv_heads >=
           (1ll << 24))
@@ -1064,8 +1064,11 @@ bool few_only(const cf_attn_desc *d) {
 // CU (1 x 1024, 32 heads on 8: 29 us against 35); with 64 columns the exponentials outweigh
 // the products and one group is always faster, with 256 two do not fit the registers.  The
 // work counts as long where the mean sequence is, or a longest one that makes a quarter of
-// all rows (chunks of 2048 among 100 decodes: 314 us with two groups, 341 with one).
+// all rows (chunks of 2048 among 100 decodes: 314 us with two groups, 341 with one).  A grid
+// of 2^23 workgroups of two groups would have 2^32 threads, which no launch takes: one group,
+// whose grid the callers' checks bound.
 int groups_of(int D, int64_t rows, int64_t longest, int n_seq, int Hkv) {
+  if ((rows / (2 * kRowsGroup) + n_seq + 4096) * Hkv >= (1ll << 23)) return 1;
   const bool is_long = rows >= 2048ll * n_seq || (longest >= 4096 && 4 * longest >= rows);
   return D > 64 && D <= 128 && is_long && rows * Hkv >= 192 * 256 ? 2 : 1;
 }

@@ -142,3 +142,21 @@ def test_many_small_weights_of_a_prompt(cf, n_q, heads, dim):
     q, k, v = _tail(n_q, heads, m, dim, n_q)
     got = cf.cf_attn_prompt(q, k, v, _i32([0, n_q]), _i32([0, m]), causal=False, scale=1.0, lse=True)
     _check_tail(got, q, k, v, [m] * n_q)
+
+
+# ------------------------------------------------------------------ more workgroups than a grid of 512 threads takes
+def test_a_million_requests(cf):
+    """1.1 million requests of one token, the bound on new tokens not known: 8.8 million workgroups
+    of either kernel.  Each request sees one key, so its output is that key's value."""
+    n, heads, dim, page = 1100000, 8, 72, 16
+    _say("a million requests")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    kc, vc = (torch.randn((64, heads, page, dim), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.ones((n, heads, dim), dtype=torch.bfloat16, device="cuda")
+    at = torch.arange(n, device="cuda")
+    plan = cf.cf_attn_plan(torch.arange(n + 1, dtype=torch.int32, device="cuda"),
+                           torch.ones(n, dtype=torch.int32, device="cuda"), n, n, heads, heads, dim)
+    out = cf.cf_attn_paged(plan, q, kc, vc, (at % 64).int()[:, None].contiguous())
+    for a in range(0, n, 64 * 1000):
+        b = min(n, a + 64 * 1000)
+        assert torch.equal(out[a:b], vc[at[a:b] % 64, :, 0]), a
