@@ -604,7 +604,8 @@ cf_status cf_attn_plan(const cf_attn_desc *d, void *stream);
  * [n_tok][n_heads] float, log of the sum of the p_k, or NULL.  Sums, the
  * softmax's maximum and sum, and outputs are kept in 32 bits; the p_k are
  * rounded to the element type for their product with the values.
- * Errors: CF_EINVAL (sizes, alignment, scale not finite and > 0, NULL arrays). */
+ * Errors: CF_EINVAL (sizes, max_pages * page over 2^31 - 65536, alignment, scale not finite and
+ * > 0, NULL arrays). */
 cf_status cf_attn_paged(const cf_attn_desc *d, const cf_kv_cache *cache, const int32_t *table_dev,
                         int32_t max_pages, const void *q_dev, int64_t q_tok, int64_t q_head, float scale,
                         void *out_dev, float *lse_dev, void *stream);
@@ -616,7 +617,7 @@ cf_status cf_attn_paged(const cf_attn_desc *d, const cf_kv_cache *cache, const i
  * causal != 0 the j-th of nq queries sees keys 0 .. nk - nq + j (the last
  * query sees all), else all.  Rows that see none, lse and rounding as in
  * cf_attn_paged.  dtype: CF_BF16 / CF_F16.
- * Errors: CF_EINVAL (sizes, alignment, scale, NULL arrays). */
+ * Errors: CF_EINVAL (sizes, n_k over 2^31 - 65536, alignment, scale, NULL arrays). */
 typedef struct cf_attn_seqs {
   int32_t n_seq, n_q, n_k;
   int32_t n_heads, n_kv_heads, head_dim, dtype, causal;

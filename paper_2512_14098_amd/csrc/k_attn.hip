@@ -1097,6 +1097,10 @@ void launch_paged(const AttnArgs &a, bool few, int groups, hipStream_t s) {
   if (!few) launch_many<T, true>(a, groups, (int64_t)a.plan.cap_items[1] * a.Hkv, s);
 }
 
+// Most keys of a sequence: the kernels' key numbers are 32-bit and run past the last key by the
+// tiles whose page ids and rows they fetch ahead (at most 32 x 4 x 33 + 16 keys).
+constexpr int64_t kMaxKeys = 0x7fffffffll - 65535;
+
 bool scale_ok(float s) { return s > 0.f && s <= 1e38f; }
 
 }  // namespace
@@ -1197,6 +1201,8 @@ extern "C" cf_status cf_attn_paged(const cf_attn_desc *d, const cf_kv_cache *cac
     return set_error(CF_EINVAL, "the cache has %d heads of %d, the descriptor %d of %d", cache->n_kv_heads,
                      cache->head_dim, d->n_kv_heads, d->head_dim);
   if (max_pages < 1 || !table_dev) return set_error(CF_EINVAL, "table: max_pages %d", max_pages);
+  if ((int64_t)max_pages * cache->page > kMaxKeys)
+    return set_error(CF_EINVAL, "table: a row of %d pages of %d is too long", max_pages, cache->page);
   if (!scale_ok(scale)) return set_error(CF_EINVAL, "scale %g is not finite and > 0", (double)scale);
   if (d->n_tok == 0) return CF_OK;
   if (!q_dev || !out_dev) return set_error(CF_EINVAL, "NULL array");
@@ -1228,8 +1234,8 @@ extern "C" cf_status cf_attn_prompt(const cf_attn_seqs *p, float scale, void *ou
   const int64_t G = p->n_heads / p->n_kv_heads;
   const int groups = groups_of(p->head_dim, p->n_q * G, 0, p->n_seq, p->n_kv_heads);
   const int64_t blocks = ((int64_t)p->n_q * G / (kRowsGroup * groups) + p->n_seq) * p->n_kv_heads;
-  if ((int64_t)p->n_q * p->n_heads > 0x7fffffffll || blocks >= (1ll << 24))
-    return set_error(CF_EINVAL, "n_q x n_heads or n_seq x n_kv_heads too large");
+  if ((int64_t)p->n_q * p->n_heads > 0x7fffffffll || blocks >= (1ll << 24) || p->n_k > kMaxKeys)
+    return set_error(CF_EINVAL, "n_q x n_heads, n_seq x n_kv_heads or n_k too large");
   if (p->n_q == 0) return CF_OK;
   if (!p->q_start_dev || !p->k_start_dev || !p->q_dev || !out_dev || (p->n_k > 0 && (!p->k_dev || !p->v_dev)))
     return set_error(CF_EINVAL, "NULL array");
