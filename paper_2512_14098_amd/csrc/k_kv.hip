@@ -221,7 +221,7 @@ extern "C" cf_status cf_kv_map(int32_t n_seq, const int32_t *ctx_len_dev, const 
   a.table = table_dev; a.q_start = q_start_dev; a.kv_len = kv_len_dev; a.pos = pos_dev;
   a.head_out = head_out_dev; a.status = status_dev; a.slot = slot_dev;
   a.n_seq = n_seq; a.page_log2 = log2_of(page); a.max_pages = max_pages; a.n_free = n_free; a.n_tok = n_tok;
-  const int blocks = n_tok > 0 ? (n_tok + kMapTokens - 1) / kMapTokens : 1;
+  const int blocks = n_tok > 0 ? (n_tok - 1) / kMapTokens + 1 : 1;
   k_kv_map<<<dim3((unsigned)blocks), dim3(kMapThreads), 0, as_stream(stream)>>>(a);
   return hip_check(hipGetLastError(), "cf_kv_map");
 }
