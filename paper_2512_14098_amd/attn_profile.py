@@ -112,12 +112,11 @@ def profile(config, component=None, batch=64, layers=32, heads=32, kv_heads=8, d
     for c in model["components"]:
         if c["kind"] != "ENC":
             continue
-        e, _ = component_tokens(model, host, c["name"])
-        if any(v.endswith("_ms") for v in c["x"]):
-            e = -(-e // 20)  # audio frames of 20 ms
-        e = np.minimum(e[:batch], 4096)  # a window of long inputs
-        if len(e) == 0:
+        x = component_tokens(model, host, c["name"])[0][:batch]
+        if len(x) == 0:
             continue
+        e = -(-x // 20) if any(v.endswith("_ms") for v in c["x"]) else x  # audio frames of 20 ms
+        e = np.minimum(e, 4096)  # a window of long inputs
         starts = torch.as_tensor(np.concatenate([[0], np.cumsum(e)]).astype(np.int32)).to(device)
         y = torch.randn((int(e.sum()), 3 * 16, 64), dtype=torch.bfloat16, device=device)
         run = lambda: [cf.cf_attn_prompt(y[:, :16], y[:, 16:32], y[:, 32:], starts, causal=False)
@@ -125,7 +124,7 @@ def profile(config, component=None, batch=64, layers=32, heads=32, kv_heads=8, d
         _timed(run)
         _, s = _timed(run)
         rows.append(dict(step="encode", component=c["name"], requests=len(e), tokens=int(e.sum()), attention_s=s,
-                         model_s=c["k"][0] + c["k"][1] * float(e.sum()) + c["k"][2] * len(e)))
+                         model_s=c["k"][0] + c["k"][1] * float(x.sum()) + c["k"][2] * len(x)))
     return rows
 
 
