@@ -18,18 +18,56 @@ import torch
 from . import cf
 from .inputs import load_config
 
+FRAME_MS, WINDOW = 20, 4096  # an audio encoder's frames, and the most it attends over at once
+PATCH_FIELD = 3  # of the trace's random numbers
 ATTRS = ("prompt", "out", "patches", "aud_in_ms", "aud_out_ms", "aud_in_tok", "aud_out_tok")
 
 
-def component_tokens(model, trace, component):
-    """Input tokens X of each request of a host trace whose type runs the component."""
+def _component_requests(model, trace, component):
+    """The requests of a host trace whose type runs the component, their X and output lengths."""
     comp = next(c for c in model["components"] if c["name"] == component)
     runs = np.array([component in t["comps"] for t in model["types"]])
     t = {a: np.asarray(trace[a], np.int64) for a in ATTRS if a in trace}
     t["aud_in_tok"], t["aud_out_tok"] = -(-t["aud_in_ms"] // 80), -(-t["aud_out_ms"] // 80)
     x = sum(t[a] for a in comp["x"])
     keep = runs[np.asarray(trace["type"])] & (x > 0)
-    return x[keep], np.maximum(t[comp.get("n_out", "out")][keep], 1)
+    return np.flatnonzero(keep), x[keep], np.maximum(t[comp.get("n_out", "out")][keep], 1)
+
+
+def component_tokens(model, trace, component):
+    """Input tokens X of each request of a host trace whose type runs the component."""
+    return _component_requests(model, trace, component)[1:]
+
+
+def image_patches(model, trace, seed, requests, device="cuda"):
+    """Patches of every image of the requests, in order.  A trace holds a request's sum; its
+    images are words 0, 1, ... of the request's block of random numbers, uniform integers."""
+    requests = np.asarray(requests, np.int64)
+    ctr, key = np.zeros((len(requests), 4), np.int64), np.zeros((len(requests), 2), np.int64)
+    ctr[:, 0], ctr[:, 1], key[:, 0] = requests, PATCH_FIELD, np.uint64(seed).view(np.int64)
+    x = cf.cf_philox_eval(torch.from_numpy(ctr).to(device), torch.from_numpy(key).to(device)).cpu().numpy()
+    lo, hi = model.get("patches_per_image", [256, 1024])
+    per = lo + ((x.view(np.uint64) >> np.uint64(32)) * np.uint64(hi - lo + 1) >> np.uint64(32)).astype(np.int64)
+    n = np.asarray(trace["n_img"], np.int64)[requests]
+    out = [per[i, :k] for i, k in enumerate(n)]
+    if [int(p.sum()) for p in out] != np.asarray(trace["patches"], np.int64)[requests].tolist():
+        raise cf.CfError("the trace's patches are not those of seed %d" % seed)
+    return np.concatenate(out) if out else np.zeros(0, np.int64)
+
+
+def encoder_sequences(model, trace, component, seed, requests, device="cuda"):
+    """Lengths of the sequences that an encoder attends over for some requests: each image on its
+    own, audio in windows of WINDOW frames, other tokens request by request."""
+    comp = next(c for c in model["components"] if c["name"] == component)
+    out = []
+    for a in comp["x"]:
+        if a == "patches":
+            out += image_patches(model, trace, seed, requests, device).tolist()
+            continue
+        ms = np.asarray(trace[a.replace("_tok", "_ms")], np.int64)[requests]
+        for n in (-(-ms // 80) if a.endswith("_tok") else -(-ms // FRAME_MS) if a.endswith("_ms") else ms).tolist():
+            out += [n] if not a.endswith("_ms") else [WINDOW] * (n // WINDOW) + [n % WINDOW]
+    return [n for n in out if n > 0]
 
 
 class PagedExecutor:
@@ -112,18 +150,18 @@ def profile(config, component=None, batch=64, layers=32, heads=32, kv_heads=8, d
     for c in model["components"]:
         if c["kind"] != "ENC":
             continue
-        x = component_tokens(model, host, c["name"])[0][:batch]
+        ids, x, _ = _component_requests(model, host, c["name"])
+        ids, x = ids[:batch], x[:batch]
         if len(x) == 0:
             continue
-        e = -(-x // 20) if any(v.endswith("_ms") for v in c["x"]) else x  # audio frames of 20 ms
-        e = np.minimum(e, 4096)  # a window of long inputs
+        e = encoder_sequences(model, host, c["name"], seed, ids, device)
         starts = torch.as_tensor(np.concatenate([[0], np.cumsum(e)]).astype(np.int32)).to(device)
-        y = torch.randn((int(e.sum()), 3 * 16, 64), dtype=torch.bfloat16, device=device)
+        y = torch.randn((sum(e), 3 * 16, 64), dtype=torch.bfloat16, device=device)
         run = lambda: [cf.cf_attn_prompt(y[:, :16], y[:, 16:32], y[:, 32:], starts, causal=False)
                        for _ in range(layers)]
         _timed(run)
         _, s = _timed(run)
-        rows.append(dict(step="encode", component=c["name"], requests=len(e), tokens=int(e.sum()), attention_s=s,
+        rows.append(dict(step="encode", component=c["name"], requests=len(x), tokens=sum(e), attention_s=s,
                          model_s=c["k"][0] + c["k"][1] * float(x.sum()) + c["k"][2] * len(x)))
     return rows
 

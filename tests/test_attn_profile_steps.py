@@ -58,3 +58,11 @@ def test_audio_is_priced_in_the_components_own_unit(calls, monkeypatch):
     assert row["model_s"] == pytest.approx(0.002 + 1e-6 * sum(ms), rel=1e-12)
     row = [r for r in _profile(A, monkeypatch, ms, batch=2) if r["component"] == "E_aud"][0]
     assert row["model_s"] == pytest.approx(0.002 + 1e-6 * sum(ms[:2]), rel=1e-12)
+
+
+def test_long_audio_is_several_windows(calls, monkeypatch):
+    """20 ms a frame, 4096 frames a window, the last one shorter; nothing is cut off."""
+    A, rec = calls
+    row = [r for r in _profile(A, monkeypatch, [1000, 4481, 150003]) if r["component"] == "E_aud"][0]
+    assert rec["prompts"][0] == [50, 225, 4096, 7501 - 4096]
+    assert row["tokens"] == 50 + 225 + 7501 and row["requests"] == 3
