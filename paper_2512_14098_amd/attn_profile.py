@@ -6,7 +6,14 @@ card is the part that depends on context lengths, the attention over the cache, 
 an executor's profile (Sec. 5.1) holds.  This module measures it: requests come from the workload's trace, an executor admits them in batches of the
 batch knob, and each iteration runs the calls that a serving step makes - cf_kv_map for the step,
 cf_kv_write and cf_attn_paged for each layer on one cf_attn_plan, cf_attn_prompt for an encoder's
-batch.  Keys, values and queries are random: only their sizes matter to the time.
+batch.  Keys, values and queries are random.  Layers and heads are the caller's: no workload holds
+them, so the seconds stand beside the latency model's and are no share of it.
+
+Layers have caches of their own, as many as make one pass over the layers read PASS_BYTES, twice
+what the last-level cache holds, before it comes back to the first: with one cache for all
+layers, small batches would be read from there, which no executor's are (16 requests of c1, 32 layers:
+a decode step of 1.35 ms, 1.31 with one cache).  Times are those of the calls in a row: where the kernels
+are shorter than the calls (4 requests: 0.70 ms for 65 of them), the calls'.
 
     python -m paper_2512_14098_amd.attn_profile --config c1 --batch 64 --layers 32
 """
@@ -19,6 +26,7 @@ from . import cf
 from .inputs import load_config
 
 FRAME_MS, WINDOW = 20, 4096  # an audio encoder's frames, and the most it attends over at once
+PASS_BYTES = 512 << 20
 PATCH_FIELD = 3  # of the trace's random numbers
 ATTRS = ("prompt", "out", "patches", "aud_in_ms", "aud_out_ms", "aud_in_tok", "aud_out_tok")
 
@@ -71,9 +79,11 @@ def encoder_sequences(model, trace, component, seed, requests, device="cuda"):
 
 
 class PagedExecutor:
-    """One executor's paged cache and the attention of its iterations."""
+    """One executor's paged cache and the attention of its iterations.  tokens: those that a step
+    reads of each layer's cache (all that it holds if not given), for the number of caches."""
 
-    def __init__(self, slots, longest, layers, heads, kv_heads, dim, page=16, dtype=torch.bfloat16, device="cuda"):
+    def __init__(self, slots, longest, layers, heads, kv_heads, dim, page=16, dtype=torch.bfloat16, device="cuda",
+                 tokens=None):
         self.layers, self.heads, self.kv_heads, self.dim, self.page = layers, heads, kv_heads, dim, page
         rows = -(-longest // page)
         n_pages = slots * rows
@@ -81,9 +91,9 @@ class PagedExecutor:
         self.free = torch.arange(n_pages, dtype=torch.int32, device=device)
         self.head = torch.zeros(1, dtype=torch.int32, device=device)
         shape = (n_pages, kv_heads, page, dim)
-        # one layer's cache serves every layer of the profile: their sizes are the same
-        self.k_cache = torch.randn(shape, dtype=dtype, device=device)
-        self.v_cache = torch.randn(shape, dtype=dtype, device=device)
+        read = 2 * (n_pages * page if tokens is None else max(int(tokens), 1)) * kv_heads * dim * dtype.itemsize
+        self.caches = [tuple(torch.randn(shape, dtype=dtype, device=device) for _ in range(2))
+                       for _ in range(max(1, min(layers, -(-PASS_BYTES // read))))]
         self.qkv = torch.empty((0, heads + 2 * kv_heads, dim), dtype=dtype, device=device)
 
     def step(self, ctx_len, new_len, n_tok, max_new):
@@ -95,9 +105,10 @@ class PagedExecutor:
                                                                self.head, n_tok)
         self.head = head
         plan = cf.cf_attn_plan(q_start, kv_len, n_tok, max_new, h, g, self.dim)
-        for _ in range(self.layers):
-            cf.cf_kv_write(x[:, h:h + g], x[:, h + g:], self.k_cache, self.v_cache, slots)
-            out = cf.cf_attn_paged(plan, x[:, :h], self.k_cache, self.v_cache, self.table)
+        for layer in range(self.layers):
+            k_cache, v_cache = self.caches[layer % len(self.caches)]
+            cf.cf_kv_write(x[:, h:h + g], x[:, h + g:], k_cache, v_cache, slots)
+            out = cf.cf_attn_paged(plan, x[:, :h], k_cache, v_cache, self.table)
         return out, status
 
 
@@ -127,7 +138,8 @@ def profile(config, component=None, batch=64, layers=32, heads=32, kv_heads=8, d
     n = len(x)
     if n == 0:
         raise cf.CfError("no request of the trace runs " + llm)
-    ex = PagedExecutor(n, int(x.max()) + decode_steps + 1, layers, heads, kv_heads, dim, page, device=device)
+    ex = PagedExecutor(n, int(x.max()) + decode_steps + 1, layers, heads, kv_heads, dim, page, device=device,
+                       tokens=int(x.sum()))
     rows = []
     ctx = torch.zeros(n, dtype=torch.int32, device=device)
     new = torch.as_tensor(x.astype(np.int32)).to(device)

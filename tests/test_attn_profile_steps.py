@@ -66,3 +66,31 @@ def test_long_audio_is_several_windows(calls, monkeypatch):
     row = [r for r in _profile(A, monkeypatch, [1000, 4481, 150003]) if r["component"] == "E_aud"][0]
     assert rec["prompts"][0] == [50, 225, 4096, 7501 - 4096]
     assert row["tokens"] == 50 + 225 + 7501 and row["requests"] == 3
+
+
+@pytest.mark.parametrize("layers,tokens,caches", [(6, None, 4), (6, 20, 6), (3, None, 3), (6, 32, 5), (1, 20, 1),
+                                                  (6, 1 << 20, 1)])
+def test_layers_have_caches_of_their_own(calls, monkeypatch, layers, tokens, caches):
+    """A pass over the layers reads caches of twice the last-level cache's bytes before it comes back
+    to one, or each layer has its own; a layer reads the cache that it wrote."""
+    A, rec = calls
+    token = 2 * 3 * 8 * 2  # bytes of keys and values
+    monkeypatch.setattr(A, "PASS_BYTES", 160 * token)
+    ex = A.PagedExecutor(2, 20, layers, 6, 3, 8, device="cpu", tokens=tokens)  # holds 2 x 2 pages of 16: 64 tokens
+    if tokens is None:
+        monkeypatch.setattr(A, "PASS_BYTES", 64 * 4 * token)
+        ex = A.PagedExecutor(2, 20, layers, 6, 3, 8, device="cpu")
+    one = torch.ones(2, dtype=torch.int32)
+    for step in range(2):
+        del rec["writes"][:], rec["reads"][:]
+        ex.step(one * (5 + step), one, 2, 1)
+        assert rec["writes"] == rec["reads"] and len(rec["reads"]) == layers
+        assert len(set(rec["reads"])) == caches and len(set(rec["reads"][:caches])) == caches
+        assert rec["reads"][caches:] == rec["reads"][:layers - caches]
+
+
+def test_profile_sizes_the_caches_by_the_batchs_tokens(calls, monkeypatch):
+    """Every layer of a small batch has its own cache."""
+    A, rec = calls
+    _profile(A, monkeypatch, [1000, 2000])
+    assert len(set(rec["reads"])) == 2
