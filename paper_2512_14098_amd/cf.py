@@ -727,8 +727,8 @@ def cf_kv_write(k, v, k_cache, v_cache, slots):
 class AttnPlan:
     """A step's attention plan (cf_attn_plan) with the lengths it was made from."""
 
-    def __init__(self, desc, q_start, kv_len, work):
-        self.c, self.q_start, self.kv_len, self.work = desc, q_start, kv_len, work
+    def __init__(self, desc, q_start, kv_len, work, stream):
+        self.c, self.q_start, self.kv_len, self.work, self.stream = desc, q_start, kv_len, work, stream
 
 
 def cf_attn_plan(q_start, kv_len, n_tok, max_new, n_heads, n_kv_heads, head_dim):
@@ -741,8 +741,9 @@ def cf_attn_plan(q_start, kv_len, n_tok, max_new, n_heads, n_kv_heads, head_dim)
     _check(_lib.cf_attn_plan_bytes(C.byref(d), C.byref(need)), "cf_attn_plan_bytes")
     work = torch.empty(need.value, dtype=torch.uint8, device=kv_len.device)
     d.work_dev, d.work_bytes = work.data_ptr(), need.value
-    _check(_lib.cf_attn_plan(C.byref(d), _stream()), "cf_attn_plan")
-    return AttnPlan(d, q_start, kv_len, work)
+    stream = _stream()
+    _check(_lib.cf_attn_plan(C.byref(d), stream), "cf_attn_plan")
+    return AttnPlan(d, q_start, kv_len, work, stream)
 
 
 def cf_attn_plan_bytes(n_seq, n_tok, max_new, n_heads, n_kv_heads, head_dim):
@@ -768,9 +769,12 @@ def cf_attn_paged(plan, q, k_cache, v_cache, table, scale=None, lse=False):
         raise CfError("table: expected [%d][max_pages]" % d.n_seq)
     out = torch.empty_like(q, memory_format=torch.contiguous_format)
     ls = torch.empty((d.n_tok, d.n_heads), dtype=torch.float32, device=q.device) if lse else None
+    stream = _stream()
+    if stream != plan.stream:  # the workspace is the binding's: it must outlive the call there
+        plan.work.record_stream(torch.cuda.current_stream())
     _check(_lib.cf_attn_paged(C.byref(d), C.byref(c), _ints(table, "table"), table.shape[1], q.data_ptr(), q.stride(0),
                               q.stride(1), d.head_dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
-                              ls.data_ptr() if lse else None, _stream()), "cf_attn_paged")
+                              ls.data_ptr() if lse else None, stream), "cf_attn_paged")
     return (out, ls) if lse else out
 
 

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_attn import DT, _i32, _paged_case, _run_paged, _sampled, _say, _want_paged, _want_prompt
+from tests.test_gpu_attn import DT, _compare, _i32, _paged_case, _run_paged, _sampled, _say, _want_paged, _want_prompt
 
 pytestmark = pytest.mark.gpu
 
@@ -160,3 +160,27 @@ def test_a_million_requests(cf):
     for a in range(0, n, 64 * 1000):
         b = min(n, a + 64 * 1000)
         assert torch.equal(out[a:b], vc[at[a:b] % 64, :, 0]), a
+
+
+# ------------------------------------------------------------------ a plan used on another stream
+def test_workspace_outlives_a_call_on_another_stream(cf):
+    """A plan made on one stream, used on another and dropped: its workspace is not handed out again
+    while that stream has not come to the call."""
+    c = _paged_case("bf16", [500], [1], 4, 2, 64, 16)
+    want = _want_paged(c, [500], [1], 0.125, "bf16")
+    q, kc, vc, table = c["q"].cuda(), c["kc"].cuda(), c["vc"].cuda(), _i32(c["table"])
+    plan = cf.cf_attn_plan(_i32(c["q_start"]), _i32(c["kv"]), 1, 1, 4, 2, 64)
+    size, at = plan.work.numel(), plan.work.data_ptr()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        got = cf.cf_attn_paged(plan, q, kc, vc, table, lse=True)
+        busy = torch.cuda.Event()
+        busy.record()
+    del plan
+    other = torch.empty(size, dtype=torch.uint8, device="cuda")
+    assert not busy.query()  # the call has not run yet
+    assert other.data_ptr() != at
+    side.synchronize()
+    _compare(*got, want)
