@@ -367,7 +367,9 @@ struct Item {
   int lo, end;                         // its keys
 };
 
-// Item `item` of the plan, if there is one and it names what exists.
+// Item `item` of the plan, if there is one and it names what exists: work_dev may hold anything,
+// a plan for other sizes or none.  Parts are multiples of 128 keys, so that a group of 16 keys lies
+// in one page; tile numbers below 2^27 keep row numbers in 32 bits.
 __device__ __forceinline__ bool read_item(const AttnArgs &a, int kind, int item, Item &it, Rows &r) {
   if (item >= min(a.plan.hdr->n_items[kind], a.plan.cap_items[kind])) return false;
   const PlanItem p = a.plan.items[kind][item];
@@ -376,10 +378,11 @@ __device__ __forceinline__ bool read_item(const AttnArgs &a, int kind, int item,
   r.q0 = clampi(p.q0, 0, a.n_tok);
   r.nq = clampi(p.nq, 0, a.n_tok - r.q0);
   r.nk = (int)min((int64_t)max(p.nk, 0), (int64_t)a.max_pages << a.page_log2);
-  if ((unsigned)p.seq >= (unsigned)a.n_seq || p.tile < 0 || p.n < 1) return false;
+  if ((unsigned)p.seq >= (unsigned)a.n_seq || (unsigned)p.tile >= 1u << 27 || p.n < 1) return false;
   if (p.n > 1) {
     if (p.part < 0 || p.part >= p.n || p.slot < 0 || p.slot > a.plan.cap_slots[kind] - p.n ||
-        (unsigned)p.join >= (unsigned)a.plan.cap_join[kind] || p.n > max_parts(kind) || len < 1 || len >= 1 << 30)
+        (unsigned)p.join >= (unsigned)a.plan.cap_join[kind] || p.n > max_parts(kind) || len < 1 || len >= 1 << 30 ||
+        (len & 127))
       return false;
     it.lo = (int)min((int64_t)p.part * len, (int64_t)1 << 30);
     if (p.part < p.n - 1) it.end = it.lo + len;
