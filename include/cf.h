@@ -522,7 +522,7 @@ cf_status cf_select_best(const double *goodput_dev, int32_t n, int32_t *best_dev
  * token s % page of page s / page.  A request's tokens are at table[request]
  * [position / page], position % page.  head_dim is a multiple of 8, 8..256;
  * pointers to elements are 16-byte aligned and strides (in elements) are
- * multiples of 8.  Lengths, page ids and starts live in device memory and are
+ * multiples of 8.  Lengths, page ids, starts and plans live in device memory and are
  * not trusted: every read and write stays inside the stated arrays whatever
  * they hold. */
 #define CF_BF16 0
@@ -538,8 +538,9 @@ typedef struct cf_kv_cache {
   int32_t dtype; /* CF_BF16 / CF_F16, also of queries, keys, values and outputs */
 } cf_kv_cache;
 
-/* Block tables and slot maps of one step from request lengths.  Request i has ctx_len_dev[i] cached tokens and
- * new_len_dev[i] new ones, packed in request order; its new pages are the next
+/* Block tables and slot maps of one step from request lengths.  Request i has
+ * ctx_len_dev[i] cached tokens and new_len_dev[i] new ones, packed in request
+ * order; its new pages are the next
  * ceil((ctx+new)/page) - ceil(ctx/page) entries of free_dev [n_free] from
  * *head_dev on, in request order, entered in its row of table_dev
  * [n_seq][max_pages] (updated in place; other entries are left).
@@ -567,12 +568,18 @@ cf_status cf_kv_write(const cf_kv_cache *cache, int32_t n_tok, const void *k_dev
 
 /* One step's attention: n_tok new tokens of n_seq requests (starts
  * q_start_dev, cached lengths with the new tokens kv_len_dev, as cf_kv_map
- * writes them; read by cf_attn_plan only), n_heads query heads, query head h reading key/value head
- * h / (n_heads / n_kv_heads).  max_new bounds a request's new tokens as far
- * as the caller knows (n_tok if it does not); it picks kernels, not results.
- * work_dev: cf_attn_plan_bytes(...) bytes, 16-byte aligned, the caller's; it
- * holds the plan and the partial results of split contexts, so calls that
- * share it must not overlap, from whichever stream. */
+ * writes them; read by cf_attn_plan only), n_heads query heads, query head h
+ * reading key/value head h / (n_heads / n_kv_heads).  max_new bounds a
+ * request's new tokens as far as the caller knows (n_tok if it does not); it
+ * picks kernels, not what they compute.  work_dev: cf_attn_plan_bytes(...)
+ * bytes, 16-byte aligned, the caller's; it holds the plan and the partial
+ * results of split contexts, so calls that share it must not overlap, from
+ * whichever stream, and cf_attn_paged takes the sizes its plan was made with.
+ * Its bytes are mostly those partial results, for as many parts as fill the
+ * GPU, whether a step's contexts are split or not: up to 18 MB where max_new
+ * leaves a request at most 16 (token, query head) rows per key/value head,
+ * else 155 MB (9 and 79 MB with 64 columns or fewer), and 48 bytes a tile of
+ * rows. */
 typedef struct cf_attn_desc {
   int32_t n_seq, n_tok, max_new;
   int32_t n_heads, n_kv_heads, head_dim;
@@ -598,8 +605,9 @@ cf_status cf_attn_plan(const cf_attn_desc *d, void *stream);
  * i, sees keys 0 .. kv_len - new + j: out = sum_k p_k v_k / sum_k p_k,
  * p_k = exp(scale q.k).  A row that sees no key (kv_len 0, or fewer keys than
  * new tokens) gives 0, and lse -inf.  Keys past kv_len are never used, whatever
- * they hold; pages outside the cache read as zeros.  Rows of tokens that no
- * request owns are left as they were.  q_dev [n_tok][n_heads][head_dim] with
+ * they hold; pages outside the cache read as zeros.  A kv_len past the table's
+ * row counts as max_pages * page (cf_kv_map refuses such a request).  Rows of
+ * tokens that no request owns are left as they were.  q_dev [n_tok][n_heads][head_dim] with
  * strides q_tok and q_head; out_dev packed; lse_dev
  * [n_tok][n_heads] float, log of the sum of the p_k, or NULL.  Sums, the
  * softmax's maximum and sum, and outputs are kept in 32 bits; the p_k are
@@ -615,8 +623,8 @@ cf_status cf_attn_paged(const cf_attn_desc *d, const cf_kv_cache *cache, const i
  * q_start_dev[i] .. q_start_dev[i+1]-1 of q_dev [n_q][n_heads][head_dim] and
  * keys k_start_dev[i] .. of k_dev, v_dev [n_k][n_kv_heads][head_dim].  With
  * causal != 0 the j-th of nq queries sees keys 0 .. nk - nq + j (the last
- * query sees all), else all.  Rows that see none, lse and rounding as in
- * cf_attn_paged.  dtype: CF_BF16 / CF_F16.
+ * query sees all), else all.  Rows that see none, rows of no sequence, lse and
+ * rounding as in cf_attn_paged.  dtype: CF_BF16 / CF_F16.
  * Errors: CF_EINVAL (sizes, n_k over 2^31 - 65536, alignment, scale, NULL arrays). */
 typedef struct cf_attn_seqs {
   int32_t n_seq, n_q, n_k;

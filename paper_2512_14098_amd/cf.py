@@ -733,7 +733,9 @@ class AttnPlan:
 
 def cf_attn_plan(q_start, kv_len, n_tok, max_new, n_heads, n_kv_heads, head_dim):
     """The plan of one step's attention, shared by the cf_attn_paged calls of all its layers.
-    max_new: the most new tokens of a request, or n_tok if not known on the host."""
+    max_new: the most new tokens of a request, or n_tok if not known on the host.  A plan holds
+    its workspace (cf_attn_plan_bytes: 17 MB for decode steps of 128 columns, 153 MB for others, also
+    for a decode step whose max_new is not known)."""
     n = kv_len.numel()
     d = cf_attn_desc(n, int(n_tok), int(max_new), int(n_heads), int(n_kv_heads), int(head_dim),
                      _ints(q_start, "q_start", n + 1), _ints(kv_len, "kv_len"), None, 0)
@@ -759,7 +761,8 @@ def cf_attn_plan_bytes(n_seq, n_tok, max_new, n_heads, n_kv_heads, head_dim):
 def cf_attn_paged(plan, q, k_cache, v_cache, table, scale=None, lse=False):
     """Attention of the step's new tokens q [n_tok][n_heads][dim] over the cache, causal within
     a request: [n_tok][n_heads][dim], with lse also the rows' log-sum-exp [n_tok][n_heads].
-    scale: head_dim ** -0.5 unless given."""
+    scale: head_dim ** -0.5 unless given.  Rows of tokens that no request owns (before the first
+    start, past the last) are not written: they hold what the allocator's memory held."""
     d = plan.c
     c = _kv_cache(k_cache, v_cache)
     q = _rows(q, "q", d.n_heads, d.head_dim, k_cache.dtype)
@@ -781,7 +784,7 @@ def cf_attn_paged(plan, q, k_cache, v_cache, table, scale=None, lse=False):
 def cf_attn_prompt(q, k, v, q_start, k_start=None, causal=True, scale=None, lse=False):
     """Attention of packed sequences: q [n_q][n_heads][dim], k and v [n_k][n_kv_heads][dim],
     starts q_start and k_start (q_start if None) [n + 1]: [n_q][n_heads][dim], with lse also
-    [n_q][n_heads]."""
+    [n_q][n_heads].  Rows outside the sequences are not written, as in cf_attn_paged."""
     k_start = q_start if k_start is None else k_start
     q = _rows(q, "q")
     n_q, heads, dim = q.shape

@@ -51,6 +51,7 @@ cf_status lower_model(const cf_model_desc *d, KModel *k);
 cf_status set_error(cf_status s, const char *fmt, ...);
 cf_status hip_check(hipError_t e, const char *what);
 hipStream_t as_stream(void *s);
+inline int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }  // x > 0, a power of two
 
 // ------------------------------------------------------------------ device primitives
 // a * m as two 64-bit words from the four 32 x 32 products: four

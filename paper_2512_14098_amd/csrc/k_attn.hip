@@ -1033,8 +1033,6 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
 }
 
 // ------------------------------------------------------------------ host
-int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
-
 cf_status check_heads(int H, int Hkv, int D) {
   if (H < 1 || Hkv < 1 || H > 65535 || H % Hkv)
     return set_error(CF_EINVAL, "n_heads %d is not a multiple of n_kv_heads %d", H, Hkv);

@@ -181,8 +181,6 @@ __global__ __launch_bounds__(256) void k_kv_write(WriteArgs a) {
   }
 }
 
-int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
-
 }  // namespace
 
 // Page sizes of the cache: powers of two, 16 to 256.
