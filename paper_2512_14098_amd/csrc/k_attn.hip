@@ -73,8 +73,8 @@ __device__ __forceinline__ i32x4 load16(const void *p) {
 }
 
 // The same without a place in the caches: a decode step reads each layer's keys and values
-// once (1.9 GB: 281 us against 315, 131 MB not read before: 29.0 against 30.5; 134 MB read
-// again and again, so that the last-level cache holds them: 36 against 33).
+// once (1.9 GB: 290 us against 320; 131 MB not read before: 28.7 against 30.4; 131 MB read again
+// and again, so that the last-level cache holds them: 27.0 against 26.9).
 __device__ __forceinline__ i32x4 load16_nt(const void *p) {
   typedef const __attribute__((address_space(1))) i32x4 *gp;
   return __builtin_nontemporal_load((gp)(uintptr_t)p);
@@ -689,15 +689,19 @@ __device__ __forceinline__ void matrix_order() {
 // one barrier a round.
 //
 // Bound by the matrix unit and its power: one causal sequence of 32767 tokens (32
-// heads on 8, 128 columns, bf16) 7.16 ms, 1.23 PFLOP/s, as a large library matrix
-// product on the same card; the unit is busy 70 % of the cycles at 1.65 GHz.  What
+// heads on 8, 128 columns, bf16) 7.09 ms, 1.24 PFLOP/s, as a large library matrix
+// product on the same card; the unit is busy 71 % of the cycles at 1.65 GHz.  What
 // the steps to it were worth on that case: a tile's work in one stream, operands
 // read right before their use, 9.6 ms; the maximum allowed to lag 8.7; two groups
 // out of step 9.5 and, with the operand reads ordered ahead, 8.1; the exponentials
 // kept in the vector phase 7.3.  Short sequences pay 8 us a workgroup to start and
-// end: 16 causal prompts of 1387 tokens on average 408 us, 0.87 PFLOP/s.  With 64
-// columns the exponentials take longer than the products: 16 full images of 623
-// patches, 16 heads, 53 us, 0.54 PFLOP/s.
+// end: 16 causal prompts of 1387 tokens on average 412 us, 0.86 PFLOP/s.  With 64
+// columns the exponentials take longer than the products, and what is neither is
+// the start, the end and the edge rounds of 4 to 16 tiles: 16 full images of 623
+// patches, 16 heads, 53 us, 0.54 PFLOP/s, matrix unit busy 36 %.  Above 128 columns a
+// wave's state does not fit the registers (32 of them spilled, 55 over a cache): one
+// causal sequence of 4096 tokens, 16 heads of 256, 241 us, 0.57 PFLOP/s; two chunks of
+// 1000 tokens on 24001, 32 heads on 8, 3.4 ms, 0.48 PFLOP/s.  136 to 248 columns take as long.
 template <typename T, int KS, int DB, int DS, int NG, bool PAGED>
 __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_attn_many(AttnArgs a) {
   using V8 = typename Elem<T>::v8;
@@ -1059,13 +1063,15 @@ bool few_only(const cf_attn_desc *d) {
 }
 
 // The many-row kernel with two groups of four waves, out of step on one CU, or with one
-// group (two or three of its workgroups on a CU).  Two are faster on long contexts (one
-// sequence of 16384, 16 heads of 128: 1880 us against 2130), one where the work is in short
-// ones (4 x 1024, 32 heads: 64 us against 78) or too little for one workgroup of 256 rows a
-// CU (1 x 1024, 32 heads on 8: 29 us against 35); with 64 columns the exponentials outweigh
-// the products and one group is always faster, with 256 two do not fit the registers.  The
-// work counts as long where the mean sequence is, or a longest one that makes a quarter of
-// all rows (chunks of 2048 among 100 decodes: 314 us with two groups, 341 with one).  A grid
+// group (two or three of its workgroups on a CU).  Two are faster on long contexts (one full
+// sequence of 16384, 16 heads of 128: 1771 us against 2079), one where the work is in short
+// ones (4 x 1024, 32 heads: 56 us against 62) or too little for one workgroup of 256 rows a
+// CU (1 x 1024, 32 heads on 8: 25 us against 30); with 64 columns one group is never slower
+// (16 images: 52 us against 67; 16384 tokens: 1164 against 1166), with 256 two do not fit the
+// registers.  The work counts as long where the mean sequence is, or a longest one that makes a
+// quarter of all rows (a chunk of 2048 on 6000 among 100 decodes: 359 us with two groups, 378
+// with one).  The packed call does not know its longest sequence and goes by the mean alone
+// (8192 tokens among 60 prompts of 100: 558 us with the one group it takes, 517 with two).  A grid
 // of 2^23 workgroups of two groups would have 2^32 threads, which no launch takes: one group,
 // whose grid the callers' checks bound.
 int groups_of(int D, int64_t rows, int64_t longest, int n_seq, int Hkv) {
