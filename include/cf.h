@@ -602,16 +602,16 @@ cf_status cf_attn_plan(const cf_attn_desc *d, void *stream);
 
 /* Attention of the new tokens over the cache, the new tokens' own keys and
  * values included (written before).  Row (t, h), the j-th new token of request
- * i, sees keys 0 .. kv_len - new + j: out = sum_k p_k v_k / sum_k p_k,
- * p_k = exp(scale q.k).  A row that sees no key (kv_len 0, or fewer keys than
- * new tokens) gives 0, and lse -inf.  Keys past kv_len are never used, whatever
- * they hold; pages outside the cache read as zeros.  A kv_len past the table's
- * row counts as max_pages * page (cf_kv_map refuses such a request).  Rows of
- * tokens that no request owns are left as they were.  q_dev [n_tok][n_heads][head_dim] with
- * strides q_tok and q_head; out_dev packed; lse_dev
- * [n_tok][n_heads] float, log of the sum of the p_k, or NULL.  Sums, the
- * softmax's maximum and sum, and outputs are kept in 32 bits; the p_k are
- * rounded to the element type for their product with the values.
+ * i, sees keys 0 .. kv_len - new + j: out = sum_k p_k v_k / sum_k p_k, p_k =
+ * exp(scale q.k).  A row that sees no key (kv_len 0, or fewer keys than new
+ * tokens), or only keys whose scores are -inf, gives 0, and lse -inf.  Keys past
+ * kv_len are never used, whatever they hold; pages outside the cache read as
+ * zeros.  A kv_len past the table's row counts as max_pages * page (cf_kv_map
+ * refuses such a request).  Rows of tokens that no request owns are left as they
+ * were.  q_dev [n_tok][n_heads][head_dim] with strides q_tok and q_head; out_dev
+ * packed; lse_dev [n_tok][n_heads] float, log of the sum of the p_k, or NULL.
+ * Sums, the softmax's maximum and sum, and outputs are kept in 32 bits; the p_k
+ * are rounded to the element type for their product with the values.
  * Errors: CF_EINVAL (sizes, max_pages * page over 2^31 - 65536, alignment, scale not finite and
  * > 0, NULL arrays). */
 cf_status cf_attn_paged(const cf_attn_desc *d, const cf_kv_cache *cache, const int32_t *table_dev,

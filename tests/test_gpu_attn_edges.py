@@ -184,3 +184,28 @@ def test_workspace_outlives_a_call_on_another_stream(cf):
     assert other.data_ptr() != at
     side.synchronize()
     _compare(*got, want)
+
+
+# ------------------------------------------------------------------ scores of minus infinity
+@pytest.mark.parametrize("new", [1, 40])
+def test_rows_whose_scores_are_all_minus_infinity(cf, new):
+    """Such rows give 0 and lse -inf, as rows that see nothing; one other key makes them its value."""
+    dim = 64
+    g = torch.Generator(device="cuda").manual_seed(new)
+    q = torch.rand((new, 2, dim), generator=g, device="cuda").add(0.5).to(torch.bfloat16)
+    k = torch.zeros((130, 1, dim), dtype=torch.bfloat16, device="cuda")
+    v = torch.randn((130, 1, dim), generator=g, device="cuda").to(torch.bfloat16)
+    k[:, :, 3] = float("-inf")
+    kc, vc = (torch.zeros((9, 1, 16, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.arange(9, dtype=torch.int32, device="cuda")[None]
+    for other in (None, 70):
+        if other is not None:
+            k[other] = 0
+        cf.cf_kv_write(k, v, kc, vc, torch.arange(130, device="cuda"))
+        plan = cf.cf_attn_plan(_i32([0, new]), _i32([130]), new, new, 2, 1, dim)
+        for out, lse in (cf.cf_attn_paged(plan, q, kc, vc, table, lse=True),
+                         cf.cf_attn_prompt(q, k, v, _i32([0, new]), _i32([0, 130]), causal=False, lse=True)):
+            if other is None:
+                assert bool((out == 0).all()) and bool(torch.isneginf(lse).all())
+            else:
+                assert torch.equal(out, v[other].expand_as(out)) and bool((lse == 0).all())
