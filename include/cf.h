@@ -635,6 +635,74 @@ typedef struct cf_attn_seqs {
 } cf_attn_seqs;
 cf_status cf_attn_prompt(const cf_attn_seqs *a, float scale, void *out_dev, float *lse_dev, void *stream);
 
+/* ------------------------------------------------------------------ rotary positions and the 8-bit cache
+ * What stands between an executor's projections and its attention, and a cache of half
+ * the bytes, so that a decode step reads, and a hand-over between executors sends, half as much.
+ *
+ * Rotary positions: the first rot_dim columns of a head are rot_dim / 2 pairs, columns (i,
+ * rot_dim / 2 + i), or (2i, 2i + 1) with interleaved != 0; the others pass.  Pair i of token t turns by
+ * phi = pos_dev[axis_dev[i]][t] * freq_dev[i] radians: (a, b) becomes (a cos phi - b sin phi,
+ * b cos phi + a sin phi), by -phi with inverse != 0 (the gradient of the turn, and its
+ * undoing up to rounding).  Text has one axis; pictures two, videos three (time, height, width).
+ * Angles, sines, cosines and products are in 64 bits, the result rounded to 32 and then to the
+ * element type.  axis_dev NULL: axis 0 for every pair.  An axis that does not exist is read as
+ * position 0; positions may be negative.
+ *
+ * Cache: one layer's keys and values, e4m3 codes [n_pages][n_kv_heads][page][head_dim] each, and
+ * a byte per row of either, [n_pages][n_kv_heads][2][page], keys' before values': the row's scale is
+ * 2^(byte - 127).  Pages and slots as above; head_dim is a multiple of 16, 16..256; pointers
+ * are 16-byte aligned.  A row x is written with the smallest scale 2^e, e >= -126, such that
+ * max |x| <= 448 * 2^e over its finite elements, and each element as the nearest code to x * 2^-e,
+ * ties to even; |x| is cut at 61440 in fp16 and 1.875 * 2^127 in bf16, so that every value held is one of the
+ * element type; reading rounds to the dtype asked for (a cache written in bf16 and read in fp16
+ * may give infinities).  Infinities and NaN are held as NaN.  The relative error of a value held
+ * is at most 2^-4 down to 2^-6 of the scale, below that at most 2^-10 of the scale. */
+typedef struct cf_kv_cache8 {
+  void *k_dev, *v_dev; /* [n_pages][n_kv_heads][page][head_dim] e4m3 */
+  uint8_t *exp_dev;    /* [n_pages][n_kv_heads][2][page] */
+  int32_t n_pages, page, n_kv_heads, head_dim;
+  int32_t dtype; /* CF_BF16 / CF_F16: of queries, keys, values and outputs */
+} cf_kv_cache8;
+
+typedef struct cf_rope_desc {
+  int32_t n_axes, rot_dim; /* 1..16; a multiple of 8, 8..head_dim */
+  int32_t interleaved, inverse;
+  const int32_t *pos_dev;  /* [n_axes][n_tok] */
+  const double *freq_dev;  /* [rot_dim / 2] */
+  const int32_t *axis_dev; /* [rot_dim / 2] or NULL */
+} cf_rope_desc;
+
+/* Queries [n_tok][n_heads][head_dim] and keys [n_tok][n_kv_heads][head_dim] (none with n_kv_heads 0) turned by
+ * their positions into q_out_dev and k_out_dev.  Strides are in elements and multiples of 8.
+ * An output may be its input, with the same strides; else outputs and inputs do not overlap.
+ * Errors: CF_EINVAL (sizes, alignment, NULL arrays, in place with other strides). */
+cf_status cf_rope(const cf_rope_desc *r, int32_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                  int32_t dtype, const void *q_dev, int64_t q_tok, int64_t q_head, void *q_out_dev, int64_t qo_tok,
+                  int64_t qo_head, const void *k_dev, int64_t k_tok, int64_t k_head, void *k_out_dev, int64_t ko_tok,
+                  int64_t ko_head, void *stream);
+
+/* cf_kv_write into the 8-bit cache.  Slots outside the cache are skipped.  The slots of a call's
+ * tokens differ: one that is given twice holds codes and a scale of either token.
+ * Errors: CF_EINVAL (sizes, alignment, NULL arrays). */
+cf_status cf_kv_write8(const cf_kv_cache8 *cache, int32_t n_tok, const void *k_dev, int64_t k_tok, int64_t k_head,
+                       const void *v_dev, int64_t v_tok, int64_t v_head, const int64_t *slot_dev, void *stream);
+
+/* Both in one launch: queries turned into q_out_dev, keys turned and written, values
+ * written, to the bit what cf_rope and cf_kv_write8 on its keys give.
+ * Errors: those of the two. */
+cf_status cf_rope_write8(const cf_rope_desc *r, const cf_kv_cache8 *cache, int32_t n_tok, int32_t n_heads,
+                         const void *q_dev, int64_t q_tok, int64_t q_head, void *q_out_dev, int64_t qo_tok,
+                         int64_t qo_head, const void *k_dev, int64_t k_tok, int64_t k_head, const void *v_dev,
+                         int64_t v_tok, int64_t v_head, const int64_t *slot_dev, void *stream);
+
+/* The cached tokens of n_seq requests as packed rows: request i's tokens 0 ..
+ * k_start_dev[i+1] - k_start_dev[i] - 1, found by its row of table_dev [n_seq][max_pages], are rows k_start_dev[i] .. of
+ * k_out_dev and v_out_dev [n_tok][n_kv_heads][head_dim], as cf_attn_prompt takes them.  Pages outside the cache
+ * and positions past the table's row read as zeros; rows of no request are left as they were.
+ * Errors: CF_EINVAL (sizes, alignment, NULL arrays). */
+cf_status cf_kv_read8(const cf_kv_cache8 *cache, const int32_t *table_dev, int32_t max_pages, int32_t n_seq,
+                      const int32_t *k_start_dev, int32_t n_tok, void *k_out_dev, void *v_out_dev, void *stream);
+
 /* Diagnostics for tests: the device primitives applied element-wise.
  * op 0: cf_log(x)  1: cf_exp(x)  2: sqrt(x)  3: x / y  4: uniform(bits of x)
  * y_dev is only read by op 3; out_dev[n]. */

@@ -88,6 +88,16 @@ class cf_kv_cache(C.Structure):
                 ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
 
 
+class cf_kv_cache8(C.Structure):
+    _fields_ = [("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("exp_dev", C.c_void_p), ("n_pages", C.c_int32),
+                ("page", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class cf_rope_desc(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("inverse", C.c_int32),
+                ("pos_dev", C.c_void_p), ("freq_dev", C.c_void_p), ("axis_dev", C.c_void_p)]
+
+
 class cf_attn_desc(C.Structure):
     _fields_ = [("n_seq", C.c_int32), ("n_tok", C.c_int32), ("max_new", C.c_int32), ("n_heads", C.c_int32),
                 ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("q_start_dev", C.c_void_p),
@@ -134,6 +144,10 @@ def _load():
         "cf_attn_plan": ([vp, vp], i32),
         "cf_attn_paged": ([vp, vp, vp, i32, vp, i64, i64, C.c_float, vp, vp, vp], i32),
         "cf_attn_prompt": ([vp, C.c_float, vp, vp, vp], i32),
+        "cf_rope": ([vp, i32, i32, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp], i32),
+        "cf_kv_write8": ([vp, i32, vp, i64, i64, vp, i64, i64, vp, vp], i32),
+        "cf_rope_write8": ([vp, vp, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp], i32),
+        "cf_kv_read8": ([vp, vp, i32, i32, vp, i32, vp, vp, vp], i32),
         "cf_math_eval": ([i32, vp, vp, vp, i64, vp], i32),
         "cf_philox_eval": ([vp, vp, vp, i64, vp], i32),
         "cf_release_scratch": ([], i32),
@@ -151,7 +165,8 @@ EXPORTED = ("cf_last_error", "cf_status_str", "cf_version", "cf_trace_gen", "cf_
             "cf_eval_mc_curve", "cf_goodput_curve", "cf_pareto",
             "cf_enum_logical", "cf_enum_count", "cf_enum_plans", "cf_enum_screen",
             "cf_goodput_reduce", "cf_select_best", "cf_kv_map", "cf_kv_write", "cf_attn_plan_bytes",
-            "cf_attn_plan", "cf_attn_paged", "cf_attn_prompt", "cf_math_eval", "cf_philox_eval", "cf_release_scratch")
+            "cf_attn_plan", "cf_attn_paged", "cf_attn_prompt", "cf_rope", "cf_kv_write8", "cf_rope_write8",
+            "cf_kv_read8", "cf_math_eval", "cf_philox_eval", "cf_release_scratch")
 
 
 def lib():
@@ -802,6 +817,134 @@ def cf_attn_prompt(q, k, v, q_start, k_start=None, causal=True, scale=None, lse=
     _check(_lib.cf_attn_prompt(C.byref(a), dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
                                ls.data_ptr() if lse else None, _stream()), "cf_attn_prompt")
     return (out, ls) if lse else out
+
+
+# ------------------------------------------------------------------ rotary positions and the 8-bit cache
+def _rope(pos, freq, axis, dim, n_tok, interleaved, inverse):
+    rot = 2 * freq.numel()
+    n_axes = 1 if pos.dim() == 1 else pos.shape[0]
+    if pos.dim() not in (1, 2) or pos.shape[-1] != n_tok:
+        raise CfError("pos: expected [%d] or [axes][%d], got %s" % (n_tok, n_tok, tuple(pos.shape)))
+    if rot > dim:
+        raise CfError("freq: %d pairs, a head has %d" % (freq.numel(), dim // 2))
+    return cf_rope_desc(n_axes, rot, int(bool(interleaved)), int(bool(inverse)), _ints(pos, "pos"),
+                        _ints(freq, "freq", dtype=torch.float64),
+                        None if axis is None else _ints(axis, "axis", freq.numel()))
+
+
+def _same_device(what, *tensors):
+    """Raw addresses carry no device, and the call runs on the current one's stream."""
+    if not all(t.is_cuda for t in tensors if t is not None):
+        raise CfError("%s: expected device tensors" % what)
+    at = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise CfError("%s: a tensor on %s, the current device is %d" % (what, t.device, at))
+
+
+def _turned(x, given, in_place, what):
+    """Where a turned tensor goes: a packed new one, or the caller's own."""
+    if not in_place:
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
+    if x is not given:
+        raise CfError("%s: in place needs rows packed within a head, 16-byte aligned, strides multiples of 8" % what)
+    return x
+
+
+def cf_rope(q, k, pos, freq, axis=None, interleaved=False, inverse=False, in_place=False):
+    """Queries and keys [n_tok][heads][dim] turned by their positions: pos int32 [n_tok] or [axes][n_tok],
+    freq float64 [pairs], radians a position, axis int32 [pairs] (the axis of each pair; axis 0
+    if None).  Pairs are columns (i, pairs + i), or (2i, 2i + 1) with interleaved; columns past the
+    pairs pass.  inverse turns back, which is the gradient's turn.  Returns (q, k) in new tensors, or with
+    in_place in the same; k may be None, and q alone is returned."""
+    x = _rows(q, "q")
+    n, heads, dim = x.shape
+    y = None if k is None else _rows(k, "k", None, dim, x.dtype)
+    if y is not None and y.shape[0] != n:
+        raise CfError("q and k: %d and %d tokens" % (n, y.shape[0]))
+    _same_device("cf_rope", x, y, pos, freq, axis)
+    r = _rope(pos, freq, axis, dim, n, interleaved, inverse)
+    xo = _turned(x, q, in_place, "q")
+    yo = None if y is None else _turned(y, k, in_place, "k")
+    ks = (None, 0, 0, None, 0, 0) if y is None else (y.data_ptr(), y.stride(0), y.stride(1), yo.data_ptr(),
+                                                     yo.stride(0), yo.stride(1))
+    _check(_lib.cf_rope(C.byref(r), n, heads, 0 if y is None else y.shape[1], dim, ATTN_DTYPE[x.dtype], x.data_ptr(),
+                        x.stride(0), x.stride(1), xo.data_ptr(), xo.stride(0), xo.stride(1), *ks, _stream()),
+           "cf_rope")
+    return xo if y is None else (xo, yo)
+
+
+def _kv_cache8(k_cache, v_cache, exps, dtype):
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
+        raise CfError("cache: expected two tensors [pages][heads][page][dim] of one shape")
+    if k_cache.dtype != torch.float8_e4m3fn or v_cache.dtype != torch.float8_e4m3fn or exps.dtype != torch.uint8:
+        raise CfError("cache: expected float8_e4m3fn codes and uint8 exponents, got %s, %s and %s"
+                      % (k_cache.dtype, v_cache.dtype, exps.dtype))
+    pages, heads, page, dim = k_cache.shape
+    if tuple(exps.shape) != (pages, heads, 2, page):
+        raise CfError("exps: expected [%d][%d][2][%d], got %s" % (pages, heads, page, tuple(exps.shape)))
+    if dtype not in ATTN_DTYPE:
+        raise CfError("expected bfloat16 or float16, got %s" % dtype)
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous() and exps.is_contiguous()):
+        raise CfError("cache: expected contiguous device tensors")
+    _same_device("cache", k_cache, v_cache, exps)
+    return cf_kv_cache8(k_cache.data_ptr(), v_cache.data_ptr(), exps.data_ptr(), pages, page, heads, dim,
+                        ATTN_DTYPE[dtype])
+
+
+def _new_rows(c, k, v, dtype):
+    k = _rows(k, "k", c.n_kv_heads, c.head_dim, dtype)
+    v = _rows(v, "v", c.n_kv_heads, c.head_dim, dtype)
+    if v.shape[0] != k.shape[0]:
+        raise CfError("k and v: %d and %d tokens" % (k.shape[0], v.shape[0]))
+    return k, v
+
+
+def cf_kv_write8(k, v, k_cache, v_cache, exps, slots):
+    """Keys and values [tokens][heads][dim] of new tokens, quantised, into their slots of the caches
+    float8_e4m3fn [pages][heads][page][dim], with exps uint8 [pages][heads][2][page], in place."""
+    c = _kv_cache8(k_cache, v_cache, exps, k.dtype)
+    k, v = _new_rows(c, k, v, k.dtype)
+    _same_device("cf_kv_write8", k, v, slots)
+    n = k.shape[0]
+    _check(_lib.cf_kv_write8(C.byref(c), n, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                             v.stride(1), _ints(slots, "slots", n, torch.int64), _stream()), "cf_kv_write8")
+
+
+def cf_rope_write8(q, k, v, pos, freq, axis, k_cache, v_cache, exps, slots, interleaved=False, in_place=False):
+    """cf_rope of q and k and cf_kv_write8 of the turned keys and the values in one launch.
+    Returns the turned queries, in a new tensor or with in_place in q; k is left as it is."""
+    c = _kv_cache8(k_cache, v_cache, exps, q.dtype)
+    x = _rows(q, "q", None, c.head_dim)
+    k, v = _new_rows(c, k, v, q.dtype)
+    n = x.shape[0]
+    if k.shape[0] != n:
+        raise CfError("q and k: %d and %d tokens" % (n, k.shape[0]))
+    _same_device("cf_rope_write8", x, k, v, pos, freq, axis, slots)
+    r = _rope(pos, freq, axis, c.head_dim, n, interleaved, False)
+    out = _turned(x, q, in_place, "q")
+    _check(_lib.cf_rope_write8(C.byref(r), C.byref(c), n, x.shape[1], x.data_ptr(), x.stride(0), x.stride(1),
+                               out.data_ptr(), out.stride(0), out.stride(1), k.data_ptr(), k.stride(0), k.stride(1),
+                               v.data_ptr(), v.stride(0), v.stride(1), _ints(slots, "slots", n, torch.int64),
+                               _stream()), "cf_rope_write8")
+    return out
+
+
+def cf_kv_read8(k_cache, v_cache, exps, table, k_start, n_tok, dtype=torch.bfloat16):
+    """The cached tokens of requests as packed rows: request i's tokens 0 .. k_start[i+1] - k_start[i] - 1
+    (table int32 [n][max_pages], k_start int32 [n + 1], n_tok rows in all).  Returns keys and values
+    [n_tok][heads][dim] as cf_attn_prompt takes them; rows of no request are not written."""
+    c = _kv_cache8(k_cache, v_cache, exps, dtype)
+    n, n_tok = k_start.numel() - 1, int(n_tok)
+    if table.dim() != 2 or table.shape[0] != n:
+        raise CfError("table: expected int32 [%d][max_pages]" % n)
+    if n_tok < 0:
+        raise CfError("n_tok %d" % n_tok)
+    _same_device("cf_kv_read8", table, k_start)
+    k, v = (torch.empty((n_tok, c.n_kv_heads, c.head_dim), dtype=dtype, device=k_cache.device) for _ in range(2))
+    _check(_lib.cf_kv_read8(C.byref(c), _ints(table, "table"), table.shape[1], n, _ints(k_start, "k_start"), n_tok,
+                            k.data_ptr(), v.data_ptr(), _stream()), "cf_kv_read8")
+    return k, v
 
 
 def cf_math_eval(op, x, y=None):

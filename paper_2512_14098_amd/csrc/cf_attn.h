@@ -35,6 +35,22 @@ struct Elem<_Float16> {
   }
 };
 
+template <int N>
+struct Int {
+  static constexpr int value = N;
+};
+
+// Two of the four e4m3 codes of a word, times a power of two, as a pair of elements.
+template <typename T>
+__device__ __forceinline__ uint32_t widen8(uint32_t codes, float scale, int half) {
+  if constexpr (__is_same(T, __bf16))
+    return half ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true))
+                : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false));
+  else
+    return half ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, true))
+                : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, false));
+}
+
 constexpr float kNegInf = -__builtin_inff();
 constexpr int kRowsSmall = 16;   // (token, head) rows of a workgroup of the few-row kernel
 constexpr int kRowsGroup = 128;  // of a group of four waves of the many-row kernel

@@ -295,11 +295,6 @@ struct Dyn {
 // The kernels' state is held by reference in lambdas: not inlined, it would be memory.
 #define CF_INLINE __attribute__((always_inline))
 
-template <int N>
-struct Int {
-  static constexpr int value = N;
-};
-
 // Infinities and NaN: exponent all ones.
 template <typename T>
 constexpr uint32_t kExpMask = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
