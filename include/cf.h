@@ -695,6 +695,14 @@ cf_status cf_rope_write8(const cf_rope_desc *r, const cf_kv_cache8 *cache, int32
                          int64_t qo_head, const void *k_dev, int64_t k_tok, int64_t k_head, const void *v_dev,
                          int64_t v_tok, int64_t v_head, const int64_t *slot_dev, void *stream);
 
+/* cf_attn_paged over the 8-bit cache: the attention of the values held, on the same plan and with the
+ * same rules.  The values are widened to the element type (exactly, where the cache was written in it)
+ * and the products are that type's, as in cf_attn_paged.
+ * Errors: those of cf_attn_paged; CF_EINVAL (cache). */
+cf_status cf_attn_paged8(const cf_attn_desc *d, const cf_kv_cache8 *cache, const int32_t *table_dev,
+                         int32_t max_pages, const void *q_dev, int64_t q_tok, int64_t q_head, float scale,
+                         void *out_dev, float *lse_dev, void *stream);
+
 /* The cached tokens of n_seq requests as packed rows: request i's tokens 0 ..
  * k_start_dev[i+1] - k_start_dev[i] - 1, found by its row of table_dev [n_seq][max_pages], are rows k_start_dev[i] .. of
  * k_out_dev and v_out_dev [n_tok][n_kv_heads][head_dim], as cf_attn_prompt takes them.  Pages outside the cache

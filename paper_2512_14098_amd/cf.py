@@ -147,6 +147,7 @@ def _load():
         "cf_rope": ([vp, i32, i32, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp], i32),
         "cf_kv_write8": ([vp, i32, vp, i64, i64, vp, i64, i64, vp, vp], i32),
         "cf_rope_write8": ([vp, vp, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp], i32),
+        "cf_attn_paged8": ([vp, vp, vp, i32, vp, i64, i64, C.c_float, vp, vp, vp], i32),
         "cf_kv_read8": ([vp, vp, i32, i32, vp, i32, vp, vp, vp], i32),
         "cf_math_eval": ([i32, vp, vp, vp, i64, vp], i32),
         "cf_philox_eval": ([vp, vp, vp, i64, vp], i32),
@@ -166,7 +167,7 @@ EXPORTED = ("cf_last_error", "cf_status_str", "cf_version", "cf_trace_gen", "cf_
             "cf_enum_logical", "cf_enum_count", "cf_enum_plans", "cf_enum_screen",
             "cf_goodput_reduce", "cf_select_best", "cf_kv_map", "cf_kv_write", "cf_attn_plan_bytes",
             "cf_attn_plan", "cf_attn_paged", "cf_attn_prompt", "cf_rope", "cf_kv_write8", "cf_rope_write8",
-            "cf_kv_read8", "cf_math_eval", "cf_philox_eval", "cf_release_scratch")
+            "cf_attn_paged8", "cf_kv_read8", "cf_math_eval", "cf_philox_eval", "cf_release_scratch")
 
 
 def lib():
@@ -773,14 +774,9 @@ def cf_attn_plan_bytes(n_seq, n_tok, max_new, n_heads, n_kv_heads, head_dim):
     return need.value
 
 
-def cf_attn_paged(plan, q, k_cache, v_cache, table, scale=None, lse=False):
-    """Attention of the step's new tokens q [n_tok][n_heads][dim] over the cache, causal within
-    a request: [n_tok][n_heads][dim], with lse also the rows' log-sum-exp [n_tok][n_heads].
-    scale: head_dim ** -0.5 unless given.  Rows of tokens that no request owns (before the first
-    start, past the last) are not written: they hold what the allocator's memory held."""
+def _attn_paged(call, name, c, plan, q, table, dtype, scale, lse):
     d = plan.c
-    c = _kv_cache(k_cache, v_cache)
-    q = _rows(q, "q", d.n_heads, d.head_dim, k_cache.dtype)
+    q = _rows(q, "q", d.n_heads, d.head_dim, dtype)
     if q.shape[0] != d.n_tok:
         raise CfError("q: expected %d tokens, got %d" % (d.n_tok, q.shape[0]))
     if table.dim() != 2 or table.shape[0] != d.n_seq:
@@ -790,10 +786,19 @@ def cf_attn_paged(plan, q, k_cache, v_cache, table, scale=None, lse=False):
     stream = _stream()
     if stream != plan.stream:  # the workspace is the binding's: it must outlive the call there
         plan.work.record_stream(torch.cuda.current_stream())
-    _check(_lib.cf_attn_paged(C.byref(d), C.byref(c), _ints(table, "table"), table.shape[1], q.data_ptr(), q.stride(0),
-                              q.stride(1), d.head_dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
-                              ls.data_ptr() if lse else None, stream), "cf_attn_paged")
+    _check(call(C.byref(d), C.byref(c), _ints(table, "table"), table.shape[1], q.data_ptr(), q.stride(0), q.stride(1),
+                d.head_dim ** -0.5 if scale is None else float(scale), out.data_ptr(), ls.data_ptr() if lse else None,
+                stream), name)
     return (out, ls) if lse else out
+
+
+def cf_attn_paged(plan, q, k_cache, v_cache, table, scale=None, lse=False):
+    """Attention of the step's new tokens q [n_tok][n_heads][dim] over the cache, causal within
+    a request: [n_tok][n_heads][dim], with lse also the rows' log-sum-exp [n_tok][n_heads].
+    scale: head_dim ** -0.5 unless given.  Rows of tokens that no request owns (before the first
+    start, past the last) are not written: they hold what the allocator's memory held."""
+    return _attn_paged(_lib.cf_attn_paged, "cf_attn_paged", _kv_cache(k_cache, v_cache), plan, q, table, k_cache.dtype,
+                       scale, lse)
 
 
 def cf_attn_prompt(q, k, v, q_start, k_start=None, causal=True, scale=None, lse=False):
@@ -945,6 +950,13 @@ def cf_kv_read8(k_cache, v_cache, exps, table, k_start, n_tok, dtype=torch.bfloa
     _check(_lib.cf_kv_read8(C.byref(c), _ints(table, "table"), table.shape[1], n, _ints(k_start, "k_start"), n_tok,
                             k.data_ptr(), v.data_ptr(), _stream()), "cf_kv_read8")
     return k, v
+
+
+def cf_attn_paged8(plan, q, k_cache, v_cache, exps, table, scale=None, lse=False):
+    """cf_attn_paged over the 8-bit cache, in q's type; the plan is the same."""
+    c = _kv_cache8(k_cache, v_cache, exps, q.dtype)
+    _same_device("cf_attn_paged8", q, table, plan.work)
+    return _attn_paged(_lib.cf_attn_paged8, "cf_attn_paged8", c, plan, q, table, q.dtype, scale, lse)
 
 
 def cf_math_eval(op, x, y=None):

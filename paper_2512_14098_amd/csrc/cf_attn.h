@@ -131,6 +131,7 @@ struct AttnArgs {
   void *out;
   float *lse;
   PlanView plan;
+  const uint8_t *exps;  // 8-bit cache
 };
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }

@@ -1,0 +1,217 @@
+// cf_attn_few8.h -- the few-row attention kernel over an 8-bit cache.
+#pragma once
+#include "cf_attn_kern.h"
+
+namespace cf {
+namespace {
+
+// As k_attn_few, with codes widened to the element type, their row's scale
+// applied, on the way into the matrix instruction (keys) and into LDS (values): the
+// attention of the values held, in that kernel's arithmetic.  A wave's tile is 64
+// keys, so that as many bytes are in flight as there.  A lane loads 16 codes of
+// a key, the two halves of which go to two products: the order of the columns within a
+// product is free as long as the queries have the same.  The exponent bytes of the
+// tile's 64 keys and values lie across the lanes, a load each.
+template <typename T, int KS, int DB, int DS>
+__global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few8(AttnArgs a) {
+  using V8 = typename Elem<T>::v8;
+  using V4 = typename Elem<T>::v4;
+  constexpr int CH = DS / 16, KP = KS / 2, NV = CH;  // 16-byte chunks of a row; loads of a key group and of a tile's values
+  __shared__ __attribute__((aligned(16))) char lds[4][64 * DS * 2];
+  __shared__ float l_m[4][16], l_l[4][16];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = (int)(blockIdx.x % (unsigned)a.Hkv), item = (int)(blockIdx.x / (unsigned)a.Hkv);
+  Item it;
+  Rows r;
+  if (!read_item(a, 0, item, it, r)) return;
+  const int n_rows = r.nq * a.G, row0 = it.tile * kRowsSmall;
+  if (row0 >= n_rows) return;
+  const int row = row0 + (lane & 15), j = min(row, n_rows - 1) / a.G, g = min(row, n_rows - 1) - j * a.G;
+  const int last_j = (min(row0 + kRowsSmall, n_rows) - 1) / a.G;
+  const int seen = r.nk - r.nq + last_j + 1;  // keys the tile's last row sees
+  const int hi = __builtin_amdgcn_readfirstlane(min(seen, it.end));
+  const int lim = r.nk - r.nq + j;  // last key the lane's row sees
+  const int all = __builtin_amdgcn_readfirstlane(r.nk - r.nq + row0 / a.G + 1);  // keys that every row sees
+
+  const int gq = lane >> 4;
+  V8 qf[KS];
+  const T *qp = (const T *)a.q + (int64_t)(r.q0 + j) * a.q_tok + (int64_t)(head * a.G + g) * a.q_head;
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) {
+    const int c = 16 * ((ks >> 1) * 4 + gq) + 8 * (ks & 1);
+    qf[ks] = __builtin_bit_cast(V8, load16(c < a.D ? (const void *)(qp + c) : (const void *)g_zeros));
+  }
+
+  const uint8_t *kc = (const uint8_t *)a.k, *vc = (const uint8_t *)a.v;
+  const int page_mask = (1 << a.page_log2) - 1;
+  const int32_t *trow = a.table + (int64_t)it.seq * a.max_pages;
+  const int n_tiles = hi > it.lo ? (hi - it.lo + 63) >> 6 : 0;
+
+  f32x4 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; d++) o[d] = f32x4{0, 0, 0, 0};
+  float m = kNegInf, l = 0.f;
+  i32x4 kr[4][KP], vr[NV];
+  uint32_t ke = 0, ve = 0;  // of key `lane` of the tile
+  int ids = 0;
+  T *vt = (T *)lds[w];
+  bool bad = false;
+
+  // the wave's tile n: page ids of 16 tiles at a time lie across the lanes
+  auto load_ids = [&](int n) {
+    const int key = it.lo + 64 * (w + 4 * (n + (lane >> 2))) + 16 * (lane & 3);
+    ids = key < hi ? trow[key >> a.page_log2] : -1;
+  };
+  auto load = [&](int n) {
+    if ((n & 15) == 0) load_ids(n);
+    const int t0 = it.lo + 64 * (w + 4 * n);
+    {
+      const int id = __builtin_amdgcn_ds_bpermute((((n & 15) << 2) + gq) << 2, ids);
+      const bool ok = (unsigned)id < (unsigned)a.n_pages && t0 + lane < r.nk;
+      const int64_t prow = (int64_t)id * a.Hkv + head;
+      const uint8_t *e = a.exps + ((prow * 2) << a.page_log2) + ((t0 + lane) & page_mask);
+      ke = load1(ok ? e : (const uint8_t *)g_zeros);
+      ve = load1(ok ? e + page_mask + 1 : (const uint8_t *)g_zeros);
+    }
+    int64_t base[4];
+    int valid[4];
+#pragma unroll
+    for (int b = 0; b < 4; b++) {
+      const int id = __builtin_amdgcn_readlane(ids, ((n & 15) << 2) + b);
+      const bool in = (unsigned)id < (unsigned)a.n_pages;
+      base[b] = ((((int64_t)(in ? id : 0) * a.Hkv + head) << a.page_log2) + ((t0 + 16 * b) & page_mask)) * a.D;
+      valid[b] = in ? r.nk - (t0 + 16 * b) : 0;  // keys of the 16 that may be read
+    }
+#pragma unroll
+    for (int b = 0; b < 4; b++)
+#pragma unroll
+      for (int kp = 0; kp < KP; kp++) {
+        const int c = kp * 4 + gq, key = lane & 15;
+        const bool ok = key < valid[b] && c * 16 < a.D;
+        kr[b][kp] = load16_nt(ok ? (const void *)(kc + base[b] + key * a.D + c * 16) : (const void *)g_zeros);
+      }
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int x = i * 64 + lane, key = x / CH, c = x % CH, b = (i * 64 / CH) >> 4;
+      const bool ok = (key & 15) < valid[b] && c * 16 < a.D;
+      vr[i] = load16_nt(ok ? (const void *)(vc + base[b] + (key & 15) * a.D + c * 16) : (const void *)g_zeros);
+    }
+  };
+
+  if (w < n_tiles) load(0);
+  for (int n = 0; w + 4 * n < n_tiles; n++) {
+    const int t0 = it.lo + 64 * (w + 4 * n);
+    f32x4 s[4];
+#pragma unroll
+    for (int b = 0; b < 4; b++) {
+      const float scale = __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute((16 * b + (lane & 15)) << 2, (int)(ke << 23)));
+      s[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++)
+        s[b] = Elem<T>::mma16(__builtin_bit_cast(V8, widen16<T>(kr[b][ks >> 1], scale, ks & 1)), qf[ks], s[b]);
+    }
+    const bool some = t0 + 64 > all && r.nk > all;  // a key that not every row sees, or none
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int x = i * 64 + lane, key = x / CH, c = x % CH;
+      const float scale = __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(key << 2, (int)(ve << 23)));
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        i32x4 y = widen16<T>(vr[i], scale, h);
+        if (some) bad |= take_specials<T>(y);
+        *(i32x4 *)(vt + key * DS + ((2 * c + h) ^ swz8<DS>(key)) * 8) = y;
+      }
+    }
+    if (w + 4 * (n + 1) < n_tiles) load(n + 1);
+    if (t0 + 64 > min(all, hi)) {
+#pragma unroll
+      for (int b = 0; b < 4; b++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const int key = t0 + 16 * b + 4 * gq + i;
+          s[b][i] = key <= lim && key < hi ? s[b][i] : kNegInf;
+        }
+    }
+    float mx = kNegInf;
+#pragma unroll
+    for (int b = 0; b < 4; b++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) mx = fmaxf(mx, s[b][i]);
+    mx = max_halves(max_rows16(mx));
+    if (__ballot(mx > m)) {
+      const float mn = fmaxf(m, mx), mu = mn == kNegInf ? 0.f : mn * a.s2;
+      const float alpha = exp2_hw(fmaf(m, a.s2, -mu));
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DB; d++) o[d] = o[d] * alpha;
+    }
+    const float mp = (m == kNegInf ? 0.f : m * a.s2) - weight_shift<T>(0);
+    V8 pf[2];
+#pragma unroll
+    for (int b = 0; b < 4; b++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const float p = exp2_hw(fmaf(s[b][i], a.s2, -mp));
+        l += p;
+        pf[b >> 1][(b & 1) * 4 + i] = (T)p;
+      }
+    __builtin_amdgcn_wave_barrier();
+    const int vrow = 4 * gq + ((lane & 15) >> 2), vcol = 4 * (lane & 3);
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+#pragma unroll
+      for (int d = 0; d < DB; d++) {
+        const int c = d * 2 + (vcol >> 3), off = vcol & 7, v0 = 32 * k + vrow, v1 = v0 + 16;
+        const V4 lo4 = read_tr<T>(vt + v0 * DS + (c ^ swz8<DS>(v0)) * 8 + off);
+        const V4 hi4 = read_tr<T>(vt + v1 * DS + (c ^ swz8<DS>(v1)) * 8 + off);
+        o[d] = Elem<T>::mma16(join8<V8>(lo4, hi4), pf[k], o[d]);
+      }
+    __builtin_amdgcn_wave_barrier();
+  }
+  l = sum_halves(sum_rows16(l));
+
+  // join the waves: o through LDS (a wave's value tile is twice as large as its 16 x DS floats)
+  const int any_bad = __syncthreads_or(bad);
+  if (gq == 0) { l_m[w][lane] = m; l_l[w][lane] = l; }
+  float *ow = (float *)lds[w];
+#pragma unroll
+  for (int d = 0; d < DB; d++) *(f32x4 *)(ow + (lane & 15) * DS + d * 16 + 4 * gq) = o[d];
+  __syncthreads();
+  const int quads = a.D / 4;
+  for (int x = threadIdx.x; x < kRowsSmall * quads; x += 256) {
+    const int rr = x / quads, d4 = x - rr * quads;
+    if (row0 + rr >= n_rows) continue;
+    float mm = kNegInf;
+#pragma unroll
+    for (int i = 0; i < 4; i++) mm = fmaxf(mm, l_m[i][rr]);
+    const float mu = mm == kNegInf ? 0.f : mm;
+    float ll = 0.f;
+    f32x4 oo = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const float f = exp2_hw((l_m[i][rr] - mu) * a.s2);
+      ll = fmaf(f, l_l[i][rr], ll);
+      oo += *(const f32x4 *)((const float *)lds[i] + rr * DS + d4 * 4) * f;
+    }
+    if (it.n > 1) {
+      const int64_t pr = ((int64_t)(it.slot + it.part) * a.Hkv + head) * kRowsSmall + rr;
+      store_part(a.plan.o[0] + pr * a.D + d4 * 4, oo[0], oo[1]);
+      store_part(a.plan.o[0] + pr * a.D + d4 * 4 + 2, oo[2], oo[3]);
+      if (d4 == 0) store_part(a.plan.ml[0] + pr * 2, mm, ll);
+    } else {
+      const int jj = (row0 + rr) / a.G, gg = row0 + rr - jj * a.G;
+      const int64_t orow = (int64_t)(r.q0 + jj) * a.H + head * a.G + gg;
+      const float inv = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
+      *(V4 *)((T *)a.out + orow * a.D + d4 * 4) = __builtin_convertvector(oo * inv, V4);
+      if (a.lse && d4 == 0) a.lse[orow] = log_sum(mm, ll, a.s2, weight_shift<T>(0));
+    }
+  }
+  if (any_bad)
+    add_specials<T, true, true>(a, r, 0, it.seq, it.n > 1 ? it.slot + it.part : -1, kRowsSmall, head, row0, min(n_rows - row0, kRowsSmall),
+                          it.lo + (max(all - it.lo, 0) & ~63), hi);
+  if (it.n > 1) join_parts<T, kRowsSmall>(a, r, it, head, row0, min(n_rows - row0, kRowsSmall), (float *)lds[0]);
+}
+
+}  // namespace
+}  // namespace cf

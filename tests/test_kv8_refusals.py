@@ -119,6 +119,36 @@ def test_read(cf, bad):
     assert _call_read(cf, C.byref(_cache(cf)), **bad) == EINVAL
 
 
+def _desc(cf, **kw):
+    return _made(cf.cf_attn_desc(), dict(n_seq=4, n_tok=9, max_new=5, n_heads=4, n_kv_heads=2, head_dim=64, q_start_dev=PTR,
+                                         kv_len_dev=PTR, work_dev=PTR, work_bytes=1 << 40), kw)
+
+
+def _call_paged(cf, d, c, table=PTR, most=4, q=PTR, tok=256, head=64, scale=0.1, out=PTR):
+    return cf.lib().cf_attn_paged8(d, c, table, most, q, tok, head, scale, out, None, None)
+
+
+@pytest.mark.parametrize("bad", BAD_CACHE + [dict(n_kv_heads=4), dict(head_dim=128)])
+def test_paged_cache(cf, bad):
+    assert _call_paged(cf, C.byref(_desc(cf)), C.byref(_cache(cf, **bad))) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(n_seq=0), dict(n_tok=-1), dict(max_new=-1), dict(n_heads=3), dict(n_kv_heads=0),
+                                 dict(head_dim=60), dict(q_start_dev=None), dict(kv_len_dev=None), dict(work_dev=None),
+                                 dict(work_dev=PTR + 8), dict(work_bytes=10)])
+def test_paged_descriptor(cf, bad):
+    assert _call_paged(cf, C.byref(_desc(cf, **bad)), C.byref(_cache(cf))) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(table=None), dict(most=0), dict(most=1 << 27), dict(q=None), dict(out=None),
+                                 dict(q=PTR + 8), dict(out=PTR + 2), dict(tok=250), dict(head=63), dict(scale=0.0),
+                                 dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan"))])
+def test_paged(cf, bad):
+    assert _call_paged(cf, C.byref(_desc(cf)), C.byref(_cache(cf)), **bad) == EINVAL
+    assert _call_paged(cf, None, C.byref(_cache(cf))) == _call_paged(cf, C.byref(_desc(cf)), None) == EINVAL
+    assert _call_paged(cf, C.byref(_desc(cf, n_tok=0)), C.byref(_cache(cf)), q=None, out=None) == OK
+
+
 def test_binding_refuses(cf):
     """Host tensors, wrong types and shapes: errors of the binding, before the library is called."""
     bf, f8 = torch.bfloat16, torch.float8_e4m3fn
