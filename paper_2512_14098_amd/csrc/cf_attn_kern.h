@@ -192,9 +192,10 @@ struct Item {
 // a plan for other sizes or none.  Parts are multiples of 128 keys, so that a group of 16 keys lies
 // in one page; tile numbers below 2^27 keep row numbers in 32 bits.
 __device__ __forceinline__ bool read_item(const AttnArgs &a, int kind, int item, Item &it, Rows &r) {
-  if (item >= min(a.plan.hdr->n_items[kind], a.plan.cap_items[kind])) return false;
-  const PlanItem p = a.plan.items[kind][item];
+  if (item >= a.plan.cap_items[kind]) return false;
+  const PlanItem p = a.plan.items[kind][item];  // beside the header, not after it
   const int len = a.plan.hdr->part[kind];
+  if (item >= a.plan.hdr->n_items[kind]) return false;
   it = Item{p.seq, p.tile, p.part, p.n, p.slot, p.join, 0, 0x7fffffff};
   r.q0 = clampi(p.q0, 0, a.n_tok);
   r.nq = clampi(p.nq, 0, a.n_tok - r.q0);
@@ -408,7 +409,8 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
 #pragma unroll
   for (int i = 0; i < NL; i++) kr[i] = vr[i] = i32x4{0, 0, 0, 0};
   [[maybe_unused]] uint32_t ke[NL] = {}, ve[NL] = {};  // 8-bit cache: the rows' exponent bytes
-  uint64_t k_at = 0, v_at = 0;  // 8-bit cache: k_at is the row's number in the head's pages, v_at not used
+  uint64_t k_at = 0, v_at = 0;
+  [[maybe_unused]] uint64_t e_at = 0;  // 8-bit cache: exponent bytes of the keys, the values' a page further
   bool bad = false;
 
   // Loads of a tile's keys or values; edge: some may not be there or the tile be past the
@@ -430,7 +432,10 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
       const int key = it.lo + 64 * n + 16 * (lane & 31);
       const bool in = (unsigned)ids < (unsigned)a.n_pages;
       if constexpr (C8) {
-        k_at = in ? (((int64_t)ids * a.Hkv + head) << a.page_log2) + (key & page_mask) : ~0ull;
+        const int64_t page = (int64_t)ids * a.Hkv + head, row = (page << a.page_log2) + (key & page_mask);
+        k_at = (uint64_t)(in ? (const uint8_t *)a.k + row * a.D : (const uint8_t *)g_zeros);
+        v_at = (uint64_t)(in ? (const uint8_t *)a.v + row * a.D : (const uint8_t *)g_zeros);
+        e_at = (uint64_t)(in ? a.exps + row + (page << a.page_log2) : (const uint8_t *)g_zeros);
       } else {
         const int64_t at = (int64_t)ids * page_elems + (int64_t)(key & page_mask) * a.D;
         k_at = (uint64_t)(in ? kc + at : (const T *)g_zeros);
@@ -460,21 +465,20 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
     }
     if (!PAGED) at += 64 * tok;
   };
-  // the same of an 8-bit cache; its addresses are made of the row number by the scalar unit
-  auto load8 = [&](i32x4 (&x)[NL], uint32_t (&xe)[NL], const void *codes, int which, int n, auto edge) CF_INLINE {
+  // the same of an 8-bit cache, with the rows' exponent bytes, e_off from where the keys' are
+  auto lane_address = [&](uint64_t x, int l) CF_INLINE {
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, l), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), l);
+    return (const uint8_t *)((uint64_t)hi << 32 | lo);
+  };
+  auto load8 = [&](i32x4 (&x)[NL], uint32_t (&xe)[NL], uint64_t where, unsigned e_off, int n, auto edge) CF_INLINE {
     const int t0 = it.lo + 64 * n;
     if (!col_ok) return;
 #pragma unroll
     for (int i = 0; i < NL; i++) {
       const int rr = i * RS + lrow;
       const int l16 = ((n & 15) << 2) + __builtin_amdgcn_readfirstlane(rr >> 4);
-      const uint32_t rlo = __builtin_amdgcn_readlane((uint32_t)k_at, l16);
-      const uint32_t rhi = __builtin_amdgcn_readlane((uint32_t)(k_at >> 32), l16);
-      const int64_t r16 = (int64_t)((uint64_t)rhi << 32 | rlo);
-      const uint8_t *cb = r16 < 0 ? (const uint8_t *)g_zeros : (const uint8_t *)codes + r16 * a.D;
-      const uint8_t *eb = r16 < 0 ? (const uint8_t *)g_zeros
-                                  : a.exps + (2 * r16 - (r16 & page_mask)) + ((int64_t)which << a.page_log2);
-      const uint8_t *p = cb + (unsigned)((rr & 15) * a.D + lcol * 16), *e = eb + (rr & 15);
+      const uint8_t *p = lane_address(where, l16) + (unsigned)((rr & 15) * a.D + lcol * 16);
+      const uint8_t *e = lane_address(e_at, l16) + (unsigned)((rr & 15) + e_off);
       if (edge.value) {
         p = t0 + rr < to_load ? p : (const uint8_t *)g_zeros;
         e = t0 + rr < to_load ? e : (const uint8_t *)g_zeros;
@@ -506,8 +510,8 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   // keys nk and values nk - 1 to registers, or from there to LDS
   auto fetch = [&](int nk, auto edge) CF_INLINE {
     if constexpr (C8) {
-      load8(kr, ke, a.k, 0, nk, edge);
-      load8(vr, ve, a.v, 1, nk - 1, edge);
+      load8(kr, ke, k_at, 0, nk, edge);
+      load8(vr, ve, v_at, page_mask + 1, nk - 1, edge);
     } else {
       load(kr, k_at, kp, a.k_tok, nk, edge);
       load(vr, v_at, vp, a.v_tok, nk - 1, edge);
@@ -637,7 +641,7 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
 #pragma unroll
     for (int i = 0; i < NL; i++) first[i] = i32x4{0, 0, 0, 0};
     [[maybe_unused]] uint32_t fe[NL] = {};
-    if constexpr (C8) load8(first, fe, a.k, 0, 0, Int<1>());
+    if constexpr (C8) load8(first, fe, k_at, 0, 0, Int<1>());
     else load(first, k_at, kp, a.k_tok, 0, Int<1>());
     fetch(1, Int<1>());
     // the queries after the first keys and values: those are waited for first

@@ -45,6 +45,8 @@ struct Split {
   int n, cost, max_parts;
 };
 
+constexpr int kClasses = 18;  // of requests, by the length of their parts
+
 // One workgroup.  Pass 1 sums the work of either kernel, (row tiles) x (keys), and the
 // parts that each candidate length gives; pass 2 takes NT requests at a time, places their
 // items by a scan and writes them, a thread per item.  Bound by the latency of its few
@@ -57,7 +59,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
   __shared__ float red[NT / 64][8];
   __shared__ int64_t red64[NT / 64];
   __shared__ int64_t l_at[NT];
-  __shared__ int l_n[NT], l_rows[NT][3];
+  __shared__ int l_n[NT], l_rows[NT][3], l_seq[NT], l_tiles[NT], l_parts[NT], l_cls[NT / 64][kClasses];
   const int tid = threadIdx.x;
   int q0 = 0, nq = 0, nk = 0;  // of the request loaded last
   auto load = [&](int i, int &tiles, int &kind, int &keys) {
@@ -140,24 +142,55 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
     nq = first_nq;
     nk = first_nk;
     if (c0 && i < n_seq) load(i, tiles, kind, keys);
-    __syncthreads();  // the items of the requests before have been written
-    l_rows[tid][0] = q0;
-    l_rows[tid][1] = nq;
-    l_rows[tid][2] = nk;
     const int parts = max((int)((unsigned)(keys + (unsigned)part[kind] - 1u) / (unsigned)part[kind]), 1);
-    // Long parts first, so that the last workgroups to start are short: three classes by the
-    // length of a part (256 decodes of 300 to 4300 keys: 436 us against 468).  Not for the
-    // many-row kernel, whose neighbouring tiles of one request share keys in the L2.
+    // Long parts first, so that the last workgroups to start are short: a stable sort by the length of a
+    // part in 16 classes (256 decodes of 300 to 4300 keys: 282 us, 292 with three classes; 8-bit cache
+    // 162 and 169).  Not for the many-row kernel, whose neighbouring tiles of one request share keys
+    // in the L2: its requests come last, in order, and after them those without tiles.
+    const int lane = tid & 63, wv = tid >> 6;
     const float most = fminf((float)part[0], w[2]), mine_len = fminf((float)keys, (float)part[0]);
-    const int cls = kind ? 3 : mine_len >= 0.67f * most ? 0 : mine_len >= 0.33f * most ? 1 : 2;
-    for (int kc = 0; kc < 4; kc++) {
-      const int k = kc / 3;
-      const bool mine = cls == kc && tiles > 0;
+    const int cls = tiles == 0 ? kClasses - 1 : kind ? kClasses - 2 : 15 - (int)(mine_len / fmaxf(most, 1.f) * 15.99f);
+    int rank = 0, n_cls = 0;  // among the wave's of the class; lane c: how many of class c
+#pragma unroll
+    for (int c = 0; c < kClasses; c++) {
+      const uint64_t same = __ballot(cls == c);
+      if (cls == c) rank = __builtin_popcountll(same & ((1ull << lane) - 1));
+      if (lane == c) n_cls = __builtin_popcountll(same);
+    }
+    __syncthreads();  // the items of the requests before have been written
+    if (lane < kClasses) l_cls[wv][lane] = n_cls;
+    __syncthreads();
+    int first = 0, all = 0;
+    if (lane < kClasses)
+#pragma unroll
+      for (int e = 0; e < NT / 64; e++) {
+        const int y = l_cls[e][lane];
+        if (e < wv) first += y;
+        all += y;
+      }
+    int incl_cls = all;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up(incl_cls, o);
+      if (lane >= o) incl_cls += y;
+    }
+    rank += __shfl(first + incl_cls - all, cls);
+    l_rows[rank][0] = q0;
+    l_rows[rank][1] = nq;
+    l_rows[rank][2] = nk;
+    l_seq[rank] = i;
+    l_tiles[rank] = tiles;
+    l_parts[rank] = parts;
+    __syncthreads();
+    tiles = l_tiles[tid];
+    const int my_parts = l_parts[tid];
+    kind = !few_only && l_rows[tid][1] * G > kRowsSmall;
+    for (int k = 0; k < 2; k++) {
+      const bool mine = kind == k && tiles > 0;
       if (!__syncthreads_or(mine)) continue;
-      const int64_t items = mine ? (int64_t)tiles * parts : 0;
-      const int64_t x = items | (parts > 1 ? (items << 40) | ((int64_t)(mine ? tiles : 0) << 52) : 0);
+      const int64_t items = mine ? (int64_t)tiles * my_parts : 0;
+      const int64_t x = items | (my_parts > 1 ? (items << 40) | ((int64_t)(mine ? tiles : 0) << 52) : 0);
       // running sums over the block
-      const int lane = tid & 63, wv = tid >> 6;
       int64_t incl = x;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -166,7 +199,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
       }
       __syncthreads();
       if (lane == 63) red64[wv] = incl;
-      l_n[tid] = mine ? parts : 0;
+      l_n[tid] = mine ? my_parts : 0;
       __syncthreads();
       int64_t before = incl - x, total = 0;
 #pragma unroll
@@ -187,7 +220,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
         const int64_t b = l_at[lo];
         const unsigned np = (unsigned)max(l_n[lo], 1), rest = (unsigned)(y - (b & low));
         const int tile = (int)(rest / np), pi = (int)(rest - tile * np);
-        PlanItem it = {c0 + lo, tile, pi, (int)np, -1, -1, l_rows[lo][0], l_rows[lo][1], l_rows[lo][2], {0, 0, 0}};
+        PlanItem it = {l_seq[lo], tile, pi, (int)np, -1, -1, l_rows[lo][0], l_rows[lo][1], l_rows[lo][2], {0, 0, 0}};
         if (np > 1) {
           it.slot = slots[k] + (int)((uint64_t)b >> 40 & 0xfff) + tile * (int)np;
           it.join = joins[k] + (int)((uint64_t)b >> 52) + tile;
@@ -464,7 +497,8 @@ void launch_few(const AttnArgs &a, int64_t blocks, hipStream_t s) {
 }
 template <typename T>
 void launch_few8(const AttnArgs &a, int64_t blocks, hipStream_t s) {
-  const dim3 g((unsigned)blocks), b(256);
+  const int64_t round = 8 * few8_heads(a.Hkv, a.page_log2);
+  const dim3 g((unsigned)((blocks + round - 1) / round * round)), b(256);
   if (a.D <= 64) k_attn_few8<T, 2, 4, 64><<<g, b, 0, s>>>(a);
   else if (a.D <= 96) k_attn_few8<T, 4, 6, 128><<<g, b, 0, s>>>(a);
   else if (a.D <= 128) k_attn_few8<T, 4, 8, 128><<<g, b, 0, s>>>(a);
