@@ -116,6 +116,7 @@ def _load():
         raise CfError("libcf.so is not built (%s); run __graft_entry__.build()" % LIB_PATH)
     L = C.CDLL(LIB_PATH)
     vp, i32, i64, u32, dbl = C.c_void_p, C.c_int32, C.c_int64, C.c_uint32, C.c_double
+    RP, CP = C.POINTER(cf_rope_desc), C.POINTER(cf_kv_cache8)
     sigs = {
         "cf_last_error": ([vp, C.c_size_t], C.c_size_t),
         "cf_status_str": ([i32], C.c_char_p),
@@ -144,11 +145,11 @@ def _load():
         "cf_attn_plan": ([vp, vp], i32),
         "cf_attn_paged": ([vp, vp, vp, i32, vp, i64, i64, C.c_float, vp, vp, vp], i32),
         "cf_attn_prompt": ([vp, C.c_float, vp, vp, vp], i32),
-        "cf_rope": ([vp, i32, i32, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp], i32),
-        "cf_kv_write8": ([vp, i32, vp, i64, i64, vp, i64, i64, vp, vp], i32),
-        "cf_rope_write8": ([vp, vp, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp], i32),
-        "cf_attn_paged8": ([vp, vp, vp, i32, vp, i64, i64, C.c_float, vp, vp, vp], i32),
-        "cf_kv_read8": ([vp, vp, i32, i32, vp, i32, vp, vp, vp], i32),
+        "cf_rope": ([RP, i32, i32, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp], i32),
+        "cf_kv_write8": ([CP, i32, vp, i64, i64, vp, i64, i64, vp, vp], i32),
+        "cf_rope_write8": ([RP, CP, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp], i32),
+        "cf_attn_paged8": ([vp, CP, vp, i32, vp, i64, i64, C.c_float, vp, vp, vp], i32),
+        "cf_kv_read8": ([CP, vp, i32, i32, vp, i32, vp, vp, vp], i32),
         "cf_math_eval": ([i32, vp, vp, vp, i64, vp], i32),
         "cf_philox_eval": ([vp, vp, vp, i64, vp], i32),
         "cf_release_scratch": ([], i32),
@@ -825,26 +826,30 @@ def cf_attn_prompt(q, k, v, q_start, k_start=None, causal=True, scale=None, lse=
 
 
 # ------------------------------------------------------------------ rotary positions and the 8-bit cache
+_E4M3 = torch.float8_e4m3fn
+
+
 def _rope(pos, freq, axis, dim, n_tok, interleaved, inverse):
-    rot = 2 * freq.numel()
-    n_axes = 1 if pos.dim() == 1 else pos.shape[0]
-    if pos.dim() not in (1, 2) or pos.shape[-1] != n_tok:
-        raise CfError("pos: expected [%d] or [axes][%d], got %s" % (n_tok, n_tok, tuple(pos.shape)))
-    if rot > dim:
-        raise CfError("freq: %d pairs, a head has %d" % (freq.numel(), dim // 2))
-    return cf_rope_desc(n_axes, rot, int(bool(interleaved)), int(bool(inverse)), _ints(pos, "pos"),
-                        _ints(freq, "freq", dtype=torch.float64),
-                        None if axis is None else _ints(axis, "axis", freq.numel()))
+    pairs, shape = freq.numel(), pos.shape
+    if len(shape) not in (1, 2) or shape[-1] != n_tok:
+        raise CfError("pos: expected [%d] or [axes][%d], got %s" % (n_tok, n_tok, tuple(shape)))
+    if 2 * pairs > dim:
+        raise CfError("freq: %d pairs, a head has %d" % (pairs, dim // 2))
+    return cf_rope_desc(1 if len(shape) == 1 else shape[0], 2 * pairs, 1 if interleaved else 0, 1 if inverse else 0,
+                        _ints(pos, "pos"), _ints(freq, "freq", None, torch.float64),
+                        None if axis is None else _ints(axis, "axis", pairs))
 
 
 def _same_device(what, *tensors):
     """Raw addresses carry no device, and the call runs on the current one's stream."""
-    if not all(t.is_cuda for t in tensors if t is not None):
-        raise CfError("%s: expected device tensors" % what)
-    at = torch._C._cuda_getDevice()
+    at = tensors[0].get_device()
     for t in tensors:
         if t is not None and t.get_device() != at:
-            raise CfError("%s: a tensor on %s, the current device is %d" % (what, t.device, at))
+            raise CfError("%s: tensors on %s and %s" % (what, tensors[0].device, t.device))
+    if at < 0:
+        raise CfError("%s: expected device tensors" % what)
+    if at != torch._C._cuda_getDevice():
+        raise CfError("%s: tensors on device %d, the current one is %d" % (what, at, torch._C._cuda_getDevice()))
 
 
 def _turned(x, given, in_place, what):
@@ -871,28 +876,26 @@ def cf_rope(q, k, pos, freq, axis=None, interleaved=False, inverse=False, in_pla
     r = _rope(pos, freq, axis, dim, n, interleaved, inverse)
     xo = _turned(x, q, in_place, "q")
     yo = None if y is None else _turned(y, k, in_place, "k")
-    ks = (None, 0, 0, None, 0, 0) if y is None else (y.data_ptr(), y.stride(0), y.stride(1), yo.data_ptr(),
-                                                     yo.stride(0), yo.stride(1))
-    _check(_lib.cf_rope(C.byref(r), n, heads, 0 if y is None else y.shape[1], dim, ATTN_DTYPE[x.dtype], x.data_ptr(),
-                        x.stride(0), x.stride(1), xo.data_ptr(), xo.stride(0), xo.stride(1), *ks, _stream()),
-           "cf_rope")
+    ks = (None, 0, 0, None, 0, 0) if y is None else (y.data_ptr(), *y.stride()[:2], yo.data_ptr(), *yo.stride()[:2])
+    _check(_lib.cf_rope(r, n, heads, 0 if y is None else y.shape[1], dim, ATTN_DTYPE[x.dtype], x.data_ptr(),
+                        *x.stride()[:2], xo.data_ptr(), *xo.stride()[:2], *ks, _stream()), "cf_rope")
     return xo if y is None else (xo, yo)
 
 
 def _kv_cache8(k_cache, v_cache, exps, dtype):
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
+    shape = k_cache.shape
+    if len(shape) != 4 or shape != v_cache.shape:
         raise CfError("cache: expected two tensors [pages][heads][page][dim] of one shape")
-    if k_cache.dtype != torch.float8_e4m3fn or v_cache.dtype != torch.float8_e4m3fn or exps.dtype != torch.uint8:
+    if k_cache.dtype != _E4M3 or v_cache.dtype != _E4M3 or exps.dtype != torch.uint8:
         raise CfError("cache: expected float8_e4m3fn codes and uint8 exponents, got %s, %s and %s"
                       % (k_cache.dtype, v_cache.dtype, exps.dtype))
-    pages, heads, page, dim = k_cache.shape
-    if tuple(exps.shape) != (pages, heads, 2, page):
+    pages, heads, page, dim = shape
+    if exps.shape != (pages, heads, 2, page):
         raise CfError("exps: expected [%d][%d][2][%d], got %s" % (pages, heads, page, tuple(exps.shape)))
     if dtype not in ATTN_DTYPE:
         raise CfError("expected bfloat16 or float16, got %s" % dtype)
     if not (k_cache.is_contiguous() and v_cache.is_contiguous() and exps.is_contiguous()):
         raise CfError("cache: expected contiguous device tensors")
-    _same_device("cache", k_cache, v_cache, exps)
     return cf_kv_cache8(k_cache.data_ptr(), v_cache.data_ptr(), exps.data_ptr(), pages, page, heads, dim,
                         ATTN_DTYPE[dtype])
 
@@ -910,10 +913,10 @@ def cf_kv_write8(k, v, k_cache, v_cache, exps, slots):
     float8_e4m3fn [pages][heads][page][dim], with exps uint8 [pages][heads][2][page], in place."""
     c = _kv_cache8(k_cache, v_cache, exps, k.dtype)
     k, v = _new_rows(c, k, v, k.dtype)
-    _same_device("cf_kv_write8", k, v, slots)
+    _same_device("cf_kv_write8", k_cache, v_cache, exps, k, v, slots)
     n = k.shape[0]
-    _check(_lib.cf_kv_write8(C.byref(c), n, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
-                             v.stride(1), _ints(slots, "slots", n, torch.int64), _stream()), "cf_kv_write8")
+    _check(_lib.cf_kv_write8(c, n, k.data_ptr(), *k.stride()[:2], v.data_ptr(), *v.stride()[:2],
+                             _ints(slots, "slots", n, torch.int64), _stream()), "cf_kv_write8")
 
 
 def cf_rope_write8(q, k, v, pos, freq, axis, k_cache, v_cache, exps, slots, interleaved=False, in_place=False):
@@ -925,13 +928,12 @@ def cf_rope_write8(q, k, v, pos, freq, axis, k_cache, v_cache, exps, slots, inte
     n = x.shape[0]
     if k.shape[0] != n:
         raise CfError("q and k: %d and %d tokens" % (n, k.shape[0]))
-    _same_device("cf_rope_write8", x, k, v, pos, freq, axis, slots)
+    _same_device("cf_rope_write8", k_cache, v_cache, exps, x, k, v, pos, freq, axis, slots)
     r = _rope(pos, freq, axis, c.head_dim, n, interleaved, False)
     out = _turned(x, q, in_place, "q")
-    _check(_lib.cf_rope_write8(C.byref(r), C.byref(c), n, x.shape[1], x.data_ptr(), x.stride(0), x.stride(1),
-                               out.data_ptr(), out.stride(0), out.stride(1), k.data_ptr(), k.stride(0), k.stride(1),
-                               v.data_ptr(), v.stride(0), v.stride(1), _ints(slots, "slots", n, torch.int64),
-                               _stream()), "cf_rope_write8")
+    _check(_lib.cf_rope_write8(r, c, n, x.shape[1], x.data_ptr(), *x.stride()[:2], out.data_ptr(), *out.stride()[:2],
+                               k.data_ptr(), *k.stride()[:2], v.data_ptr(), *v.stride()[:2],
+                               _ints(slots, "slots", n, torch.int64), _stream()), "cf_rope_write8")
     return out
 
 
@@ -945,9 +947,9 @@ def cf_kv_read8(k_cache, v_cache, exps, table, k_start, n_tok, dtype=torch.bfloa
         raise CfError("table: expected int32 [%d][max_pages]" % n)
     if n_tok < 0:
         raise CfError("n_tok %d" % n_tok)
-    _same_device("cf_kv_read8", table, k_start)
+    _same_device("cf_kv_read8", k_cache, v_cache, exps, table, k_start)
     k, v = (torch.empty((n_tok, c.n_kv_heads, c.head_dim), dtype=dtype, device=k_cache.device) for _ in range(2))
-    _check(_lib.cf_kv_read8(C.byref(c), _ints(table, "table"), table.shape[1], n, _ints(k_start, "k_start"), n_tok,
+    _check(_lib.cf_kv_read8(c, _ints(table, "table"), table.shape[1], n, _ints(k_start, "k_start"), n_tok,
                             k.data_ptr(), v.data_ptr(), _stream()), "cf_kv_read8")
     return k, v
 
@@ -955,7 +957,7 @@ def cf_kv_read8(k_cache, v_cache, exps, table, k_start, n_tok, dtype=torch.bfloa
 def cf_attn_paged8(plan, q, k_cache, v_cache, exps, table, scale=None, lse=False):
     """cf_attn_paged over the 8-bit cache, in q's type; the plan is the same."""
     c = _kv_cache8(k_cache, v_cache, exps, q.dtype)
-    _same_device("cf_attn_paged8", q, table, plan.work)
+    _same_device("cf_attn_paged8", k_cache, v_cache, exps, q, table, plan.work)
     return _attn_paged(_lib.cf_attn_paged8, "cf_attn_paged8", c, plan, q, table, q.dtype, scale, lse)
 
 

@@ -35,6 +35,9 @@ struct Elem<_Float16> {
   }
 };
 
+// The kernels' state is held by reference in lambdas: not inlined, it would be memory.
+#define CF_INLINE __attribute__((always_inline))
+
 template <int N>
 struct Int {
   static constexpr int value = N;

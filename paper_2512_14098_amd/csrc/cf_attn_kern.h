@@ -101,8 +101,6 @@ __device__ __forceinline__ int swz8(int row) {
 struct Dyn {
   int value;
 };
-// The kernels' state is held by reference in lambdas: not inlined, it would be memory.
-#define CF_INLINE __attribute__((always_inline))
 
 // Half j of 16 e4m3 codes, times their row's scale, as eight elements.
 template <typename T>

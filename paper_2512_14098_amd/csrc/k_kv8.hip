@@ -76,10 +76,9 @@ __device__ __forceinline__ uint2 quantise(float (&x)[8], uint32_t &byte) {
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       const float y = fabsf(x[i]);
-      if (y < __builtin_inff()) {
-        x[i] = fminf(fmaxf(x[i], -kTop), kTop);
-        m = fmaxf(m, fminf(y, kTop));
-      }
+      const bool fine = y < __builtin_inff();
+      m = fmaxf(m, fine ? fminf(y, kTop) : 0.f);
+      x[i] = fine ? fminf(fmaxf(x[i], -kTop), kTop) : x[i];
     }
   }
   m = max_group<L>(m);
@@ -94,21 +93,70 @@ __device__ __forceinline__ uint2 quantise(float (&x)[8], uint32_t &byte) {
   return make_uint2((uint32_t)lo, (uint32_t)hi);
 }
 
-// One token's rows (queries, keys, values) by one wave or four, a row by L lanes of eight elements each:
-// four pairs where they turn, so that a turn needs no other lane's elements and may be done in place.
-// The token's sines and cosines are computed once by each wave, passed through LDS and kept
-// in registers over its rows.
-template <typename T, int L, bool ROPE, bool Q8>
+// How columns are paired: no turn; i and rot / 2 + i, the halves cut in 16 bytes or not; 2i and 2i + 1.
+enum Pairs { kNone, kHalves, kApart, kNeighbours };
+
+// A lane's eight elements: in a row, but four and four `apart` bytes away in kApart.
+template <Pairs P>
+__device__ __forceinline__ uint4 load_row(const void *p, int apart) {
+  if (P != kApart) return *(const uint4 *)p;
+  const uint2 x = *(const uint2 *)p, y = *(const uint2 *)((const char *)p + apart);
+  return make_uint4(x.x, x.y, y.x, y.y);
+}
+template <Pairs P>
+__device__ __forceinline__ void store_row(void *p, int apart, const uint4 &x) {
+  if (P == kApart) {
+    *(uint2 *)p = make_uint2(x.x, x.y);
+    *(uint2 *)((char *)p + apart) = make_uint2(x.z, x.w);
+  } else {
+    *(uint4 *)p = x;
+  }
+}
+
+// x of the lane next to this one in a pair of lanes
+__device__ __forceinline__ uint32_t neighbour(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 15, 15, true);
+}
+// kHalves: of two lanes the even one holds eight elements of the first half and the odd one those that
+// they are paired with.  They exchange four, so that each has four pairs, and back: 16-byte loads and
+// stores where four and four elements would be loaded and stored (335 MB turned 129 us, 147 with 8 bytes).
+__device__ __forceinline__ uint4 meet(const uint4 &x, bool odd) {
+  const uint32_t a = neighbour(odd ? x.x : x.z), b = neighbour(odd ? x.y : x.w);
+  return odd ? make_uint4(a, b, x.z, x.w) : make_uint4(x.x, x.y, a, b);
+}
+
+template <typename T>
+__device__ __forceinline__ void widen_row(const uint4 &x, float (&e)[8]) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    e[2 * i] = widen<T>(w[i] & 0xffff);
+    e[2 * i + 1] = widen<T>(w[i] >> 16);
+  }
+}
+
+// One token's rows (queries, then keys, then values) by one wave, or by four where tokens are few, a row by L
+// lanes of eight elements each: four pairs where they turn.  A wave has read all of a row when it writes
+// it, so that a turn may be done in place.  The token's sines and cosines are computed once by each wave,
+// passed through LDS and kept in registers over its rows.
+//
+// Bound by memory: 32,767 tokens of 32 + 8 heads of 128 turned in 129 us, 5.2 TB/s read and written (a
+// large copy: 4.8 to 5.1), 52,808 tokens of 2 x 8 heads quantised in 71 us, 5.2 TB/s, both in one launch over 22,190
+// tokens 128 us, 4.9 TB/s.  The 64-bit products are hidden behind that as long as the rest is short: with one loop over
+// all rows that asks each for its kind 150, 72 and 152 us.
+template <typename T, int L, Pairs P, bool Q8>
 __global__ __launch_bounds__(256) void k_turn(TurnArgs a) {
+  constexpr bool ROPE = P != kNone;
   __shared__ double2 l_cs[4][ROPE ? 128 : 1];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int u = lane & (L - 1), per_pass = 64 / L * a.waves;
   const int r_first = (w & (a.waves - 1)) * (64 / L) + lane / L;
   const int tokens = 4 / a.waves;  // of a workgroup
-  const int n_rows = a.Hq + a.Hk + (Q8 ? a.Hk : 0), half = a.rot / 2;
+  const int half = a.rot / 2;
   const bool has = u * 8 < a.D, turns = ROPE && u * 8 < a.rot;
-  const int oa_turn = turns && !a.interleaved ? 4 * u : 8 * u;
-  const int ob_turn = turns && !a.interleaved ? half + 4 * u : 8 * u + 4;
+  const bool pairs = P == kHalves && turns, split = P == kApart && turns, odd = u & 1;
+  // the lane's first element; bytes to its fifth
+  const int oa = pairs ? (odd ? half + 4 * (u - 1) : 4 * u) : split ? 4 * u : 8 * u, apart = split ? 2 * half : 8;
   for (int64_t t = (int64_t)blockIdx.x * tokens + w / a.waves; t < a.n_tok; t += (int64_t)gridDim.x * tokens) {
     int64_t slot = -1;
     if (Q8) slot = a.slot[t];
@@ -132,59 +180,89 @@ __global__ __launch_bounds__(256) void k_turn(TurnArgs a) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
-    const bool held = Q8 && slot >= 0 && slot < a.n_slots;
+    // turned rows: pairs (e[i], e[i + 4]), or (e[2i], e[2i + 1]), as elements and as the type's values
+    auto turn = [&](uint4 &x) CF_INLINE {
+      if (P == kHalves) {
+        const uint4 y = meet(x, odd);
+        if (turns) x = y;
+      }
+      float e[8];
+      widen_row<T>(x, e);
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        float &p = e[P == kNeighbours ? 2 * i : i], &q = e[P == kNeighbours ? 2 * i + 1 : i + 4];
+        const double dp = p, dq = q;
+        p = (float)fma(dp, c[i], -(dq * s[i]));
+        q = (float)fma(dq, c[i], dp * s[i]);
+      }
+      if (turns)  // else as they are, infinities and NaN too
+        x = make_uint4(pack2<T>(e[0], e[1]), pack2<T>(e[2], e[3]), pack2<T>(e[4], e[5]), pack2<T>(e[6], e[7]));
+    };
+    // rows that are turned and stored
+    auto turn_rows = [&](int n, const void *in, int64_t tok, int64_t head, void *out, int64_t otok, int64_t ohead) CF_INLINE {
+      const T *src = (const T *)in + t * tok + r_first * head + oa;
+      T *dst = (T *)out + t * otok + r_first * ohead + oa;
+      for (int r0 = 0; r0 < n; r0 += per_pass) {
+        const bool on = has && r0 + r_first < n;
+        if (P == kHalves) {  // every lane takes part in the exchange
+          uint4 x = make_uint4(0, 0, 0, 0);
+          if (on) x = load_row<P>(src, apart);
+          turn(x);
+          const uint4 y = meet(x, odd);  // its own inverse
+          if (turns) x = y;
+          if (on) store_row<P>(dst, apart, x);
+        } else if (on) {
+          uint4 x = load_row<P>(src, apart);
+          turn(x);
+          store_row<P>(dst, apart, x);
+        }
+        src += per_pass * head;
+        dst += per_pass * ohead;
+      }
+    };
+    // rows that go to the cache; which: 0 keys, 1 values
     const int64_t page = slot >> a.page_log2, off = slot & ((1ll << a.page_log2) - 1);
-    for (int r0 = 0; r0 < n_rows; r0 += per_pass) {
-      const int r = r0 + r_first;
-      const int kind = r < a.Hq ? 0 : r < a.Hq + a.Hk ? 1 : 2;
-      const int h = kind == 0 ? r : kind == 1 ? r - a.Hq : r - a.Hq - a.Hk;
-      const bool keep = Q8 && kind > 0;  // goes to the cache
-      const bool on = r < n_rows && has && (!keep || held);
-      const T *src = kind == 0   ? (const T *)a.q + t * a.q_tok + h * a.q_head
-                     : kind == 1 ? (const T *)a.k + t * a.k_tok + h * a.k_head
-                                 : (const T *)a.v + t * a.v_tok + h * a.v_head;
-      const int oa = kind < 2 ? oa_turn : 8 * u, ob = kind < 2 ? ob_turn : 8 * u + 4;
-      uint2 xa = make_uint2(0, 0), xb = xa;
-      if (on) {
-        xa = *(const uint2 *)(src + oa);
-        xb = *(const uint2 *)(src + ob);
-      }
-      if (ROPE && turns && kind < 2) {
-        float e[8] = {widen<T>(xa.x & 0xffff), widen<T>(xa.x >> 16), widen<T>(xa.y & 0xffff), widen<T>(xa.y >> 16),
-                      widen<T>(xb.x & 0xffff), widen<T>(xb.x >> 16), widen<T>(xb.y & 0xffff), widen<T>(xb.y >> 16)};
-        auto turn = [&](float &p, float &q, int i) {
-          const double x = p, y = q;
-          p = (float)fma(x, c[i], -(y * s[i]));
-          q = (float)fma(y, c[i], x * s[i]);
-        };
-        if (a.interleaved) {
-#pragma unroll
-          for (int i = 0; i < 4; i++) turn(e[2 * i], e[2 * i + 1], i);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; i++) turn(e[i], e[i + 4], i);
-        }
-        xa = make_uint2(pack2<T>(e[0], e[1]), pack2<T>(e[2], e[3]));
-        xb = make_uint2(pack2<T>(e[4], e[5]), pack2<T>(e[6], e[7]));
-      }
-      if (on && !keep) {
-        T *dst = kind == 0 ? (T *)a.q_out + t * a.qo_tok + h * a.qo_head : (T *)a.k_out + t * a.ko_tok + h * a.ko_head;
-        *(uint2 *)(dst + oa) = xa;
-        *(uint2 *)(dst + ob) = xb;
-      }
-      if (Q8 && __ballot(keep)) {
-        float x[8] = {widen<T>(xa.x & 0xffff), widen<T>(xa.x >> 16), widen<T>(xa.y & 0xffff), widen<T>(xa.y >> 16),
-                      widen<T>(xb.x & 0xffff), widen<T>(xb.x >> 16), widen<T>(xb.y & 0xffff), widen<T>(xb.y >> 16)};
+    auto hold_rows = [&](auto which, const void *in, int64_t tok, int64_t head, uint8_t *codes) CF_INLINE {
+      constexpr bool K = which.value == 0;
+      constexpr Pairs PR = K ? P : kNone;
+      const int o0 = K ? oa : 8 * u;
+      const T *src = (const T *)in + t * tok + r_first * head + o0;
+      for (int r0 = 0; r0 < a.Hk; r0 += per_pass) {
+        const int h = r0 + r_first;
+        const bool on = has && h < a.Hk;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (on) x = load_row<PR>(src, apart);
+        if (PR != kNone) turn(x);
+        float e[8];
+        widen_row<T>(x, e);
         uint32_t byte;
-        const uint2 code = quantise<T, L>(x, byte);
-        if (keep && on) {
-          const int64_t row = page * a.Hk + h;
-          uint8_t *dst = (kind == 1 ? a.kc : a.vc) + ((row << a.page_log2) + off) * a.D;
-          *(uint32_t *)(dst + oa) = code.x;
-          *(uint32_t *)(dst + ob) = code.y;
-          if (u == 0) a.ec[((row * 2 + (kind - 1)) << a.page_log2) + off] = (uint8_t)byte;
+        uint2 code = quantise<T, L>(e, byte);
+        if (PR == kHalves) {
+          const uint32_t got = neighbour(odd ? code.x : code.y);
+          if (turns) code = odd ? make_uint2(got, code.y) : make_uint2(code.x, got);
         }
+        if (on) {
+          const int64_t row = page * a.Hk + h;
+          uint8_t *dst = codes + ((row << a.page_log2) + off) * a.D + o0;
+          if (PR == kApart && split) {
+            *(uint32_t *)dst = code.x;
+            *(uint32_t *)(dst + half) = code.y;
+          } else {
+            *(uint2 *)dst = code;
+          }
+          if (u == 0) a.ec[((row * 2 + which.value) << a.page_log2) + off] = (uint8_t)byte;
+        }
+        src += per_pass * head;
       }
+    };
+    if (ROPE) turn_rows(a.Hq, a.q, a.q_tok, a.q_head, a.q_out, a.qo_tok, a.qo_head);
+    if constexpr (Q8) {
+      if (slot >= 0 && slot < a.n_slots) {
+        hold_rows(Int<0>(), a.k, a.k_tok, a.k_head, a.kc);
+        hold_rows(Int<1>(), a.v, a.v_tok, a.v_head, a.vc);
+      }
+    } else {
+      turn_rows(a.Hk, a.k, a.k_tok, a.k_head, a.k_out, a.ko_tok, a.ko_head);
     }
   }
 }
@@ -200,7 +278,8 @@ constexpr int kReadTokens = 16;
 
 // Each wave finds the requests and pages of a quarter of the workgroup's tokens, 64 starts at
 // a time; then a thread takes 16 codes of one token's head a step, keys before values.
-template <typename T>
+// Bound by memory: 113,000 tokens of 64 requests, 2 x 8 heads of 128, in 137 us, 5.3 TB/s read and written.
+template <typename T, int U>
 __global__ __launch_bounds__(256) void k_kv_read8(ReadArgs a) {
   __shared__ int32_t l_page[kReadTokens], l_off[kReadTokens];  // page -1: zeros, -2: nobody's token
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -235,7 +314,6 @@ __global__ __launch_bounds__(256) void k_kv_read8(ReadArgs a) {
     }
     __syncthreads();
     const unsigned total = (unsigned)n_here * per_tok;
-    constexpr int U = 4;
     for (unsigned x0 = tid; x0 < total; x0 += 256 * U) {
       uint4 code[U];
       uint32_t byte[U];
@@ -255,7 +333,11 @@ __global__ __launch_bounds__(256) void k_kv_read8(ReadArgs a) {
         dst[i] = (T *)(is_v ? a.v_out : a.k_out) + ((t0 + at) * a.Hkv + h) * a.D + c * 16;
         if (page < 0) continue;
         const int64_t row = (int64_t)page * a.Hkv + h;
-        code[i] = *(const uint4 *)((is_v ? a.vc : a.kc) + ((row << a.page_log2) + off) * a.D + c * 16);
+        // read once: without a place in the caches (719 MB: 152 us against 162 with 16 tokens a workgroup)
+        typedef uint32_t V4 __attribute__((ext_vector_type(4)));
+        const V4 y = __builtin_nontemporal_load(
+            (const V4 *)((is_v ? a.vc : a.kc) + ((row << a.page_log2) + off) * a.D + c * 16));
+        code[i] = make_uint4(y[0], y[1], y[2], y[3]);
         byte[i] = a.ec[((row * 2 + is_v) << a.page_log2) + off];
       }
 #pragma unroll
@@ -277,14 +359,19 @@ __global__ __launch_bounds__(256) void k_kv_read8(ReadArgs a) {
 template <typename T, int L>
 void launch_turn(const TurnArgs &a, bool rope, bool q8, unsigned blocks, hipStream_t s) {
   const dim3 g(blocks), b(256);
-  if (rope && q8) k_turn<T, L, true, true><<<g, b, 0, s>>>(a);
-  else if (rope) k_turn<T, L, true, false><<<g, b, 0, s>>>(a);
-  else k_turn<T, L, false, true><<<g, b, 0, s>>>(a);
+  if (!rope) k_turn<T, L, kNone, true><<<g, b, 0, s>>>(a);
+  else if (a.interleaved && q8) k_turn<T, L, kNeighbours, true><<<g, b, 0, s>>>(a);
+  else if (a.interleaved) k_turn<T, L, kNeighbours, false><<<g, b, 0, s>>>(a);
+  else if (a.rot % 16 && q8) k_turn<T, L, kApart, true><<<g, b, 0, s>>>(a);
+  else if (a.rot % 16) k_turn<T, L, kApart, false><<<g, b, 0, s>>>(a);
+  else if (q8) k_turn<T, L, kHalves, true><<<g, b, 0, s>>>(a);
+  else k_turn<T, L, kHalves, false><<<g, b, 0, s>>>(a);
 }
 
 void launch(TurnArgs &a, int dtype, bool rope, bool q8, hipStream_t s) {
-  // four waves a token where the tokens are few
-  a.waves = a.n_tok < 2048 ? 4 : 1;
+  // Four waves a token where the tokens are few: 256 tokens of 40 heads turned in 5.1 us, with one wave 7.6;
+  // 700 in 7.4 and 9.1, 1500 in 10.5 and 11.0 (turned and written 13.0 and 12.7), 5000 in 23 and 19.
+  a.waves = a.n_tok < 1500 ? 4 : 1;
   const int64_t tokens = 4 / a.waves, need = ((int64_t)a.n_tok + tokens - 1) / tokens;
   const unsigned blocks = (unsigned)(need < (1 << 20) ? need : 1 << 20);
   if (dtype == CF_BF16) {
@@ -437,10 +524,19 @@ extern "C" cf_status cf_kv_read8(const cf_kv_cache8 *cache, const int32_t *table
   a.k_out = k_out_dev; a.v_out = v_out_dev;
   a.n_seq = n_seq; a.n_tok = n_tok; a.max_pages = max_pages; a.n_pages = cache->n_pages;
   a.Hkv = cache->n_kv_heads; a.D = cache->head_dim; a.page_log2 = log2_of(cache->page);
-  a.tokens = n_tok < 1024 * kReadTokens ? 4 : kReadTokens;
+  // About 1024 loads a workgroup (113,000 tokens of 2 x 8 heads of 128, 8 tokens: 137 us, with 4 146, with 16
+  // 143; heads of 64, 16 tokens: 76 us, with 8 83), less where that leaves CUs without one.
+  const int loads = cache->n_kv_heads * (cache->head_dim / 8);  // of a token
+  a.tokens = n_tok < 16384 || loads >= 512 ? 4 : loads >= 128 ? 8 : kReadTokens;
   const int64_t need = ((int64_t)n_tok + a.tokens - 1) / a.tokens;
   const dim3 g((unsigned)(need < (1 << 20) ? need : 1 << 20)), b(256);
-  if (cache->dtype == CF_BF16) k_kv_read8<__bf16><<<g, b, 0, as_stream(stream)>>>(a);
-  else k_kv_read8<_Float16><<<g, b, 0, as_stream(stream)>>>(a);
+  const hipStream_t s = as_stream(stream);
+  if (cache->dtype == CF_BF16) {
+    if (a.tokens == 4) k_kv_read8<__bf16, 4><<<g, b, 0, s>>>(a);
+    else k_kv_read8<__bf16, 8><<<g, b, 0, s>>>(a);
+  } else {
+    if (a.tokens == 4) k_kv_read8<_Float16, 4><<<g, b, 0, s>>>(a);
+    else k_kv_read8<_Float16, 8><<<g, b, 0, s>>>(a);
+  }
   return hip_check(hipGetLastError(), "cf_kv_read8");
 }
