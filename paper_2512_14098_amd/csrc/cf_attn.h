@@ -57,7 +57,6 @@ __device__ __forceinline__ uint32_t widen8(uint32_t codes, float scale, int half
 constexpr float kNegInf = -__builtin_inff();
 constexpr int kRowsSmall = 16;   // (token, head) rows of a workgroup of the few-row kernel
 constexpr int kRowsGroup = 128;  // of a group of four waves of the many-row kernel
-constexpr int kMinPart = 256;    // fewest keys of a part of a split context
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 

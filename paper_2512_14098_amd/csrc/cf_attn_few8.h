@@ -26,14 +26,19 @@ __host__ __device__ inline unsigned few8_heads(int Hkv, int page_log2) {
 // Leaving out the conversions, the products or the stores to LDS changes no time.  Three
 // workgroups a CU (161 registers) hold as much in flight as two of tiles of 64 keys (236
 // registers), which take 162 us and 52.
-template <typename T, int KS, int DB, int DS>
-__global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few8(AttnArgs a) {
+template <typename T, int KS, int DB, int DS, bool JOIN>
+__global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few8(AttnArgs a, int own_blocks, int join_rows) {
   using V8 = typename Elem<T>::v8;
   using V4 = typename Elem<T>::v4;
   constexpr int CH = DS / 16, KP = KS / 2, NV = 32 * CH / 64;  // chunks of a row, loads of 16 keys and of 32 values
   __shared__ __attribute__((aligned(16))) char lds[4][32 * DS * 2];
+  static_assert(sizeof(JoinLds) <= sizeof(lds), "");
   __shared__ float l_m[4][16], l_l[4][16];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (JOIN && (int)blockIdx.x >= own_blocks) {
+    join_many<T>(a, join_rows, (int)blockIdx.x - own_blocks, *(JoinLds *)lds[0]);
+    return;
+  }
   // Workgroups go round the XCDs, each with an L2 of its own.  The heads whose exponent bytes share a line
   // follow each other on one XCD, so that it need not be fetched by each (64 columns 79 us against 81).
   const unsigned hg = few8_heads(a.Hkv, a.page_log2), units = (unsigned)a.Hkv / hg;
@@ -236,7 +241,7 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few8(AttnArgs a)
   if (any_bad)
     add_specials<T, true, true>(a, r, 0, it.seq, it.n > 1 ? it.slot + it.part : -1, kRowsSmall, head, row0, min(n_rows - row0, kRowsSmall),
                           it.lo + (max(all - it.lo, 0) & ~31), hi);
-  if (it.n > 1) join_parts<T, kRowsSmall>(a, r, it, head, row0, min(n_rows - row0, kRowsSmall), (float *)lds[0]);
+  if (it.n > 1) join_parts<T>(a, r, it, head, row0, min(n_rows - row0, kRowsSmall), (float *)lds[0]);
 }
 
 }  // namespace

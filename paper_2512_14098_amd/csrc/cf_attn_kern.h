@@ -59,7 +59,9 @@ __device__ __forceinline__ float log_sum(float m, float l, float s2, float shift
 }
 
 // Most parts of one context: their weights for a tile's rows are held in LDS.
-__host__ __device__ constexpr int max_parts(int kind) { return kind ? 16 : 128; }
+__host__ __device__ constexpr int max_parts(int kind) { return kind ? 64 : 128; }
+// Fewest keys of a part (many rows, 40 tokens on 1000: 22 us, 29 with 256).
+__host__ __device__ constexpr int min_part(int kind) { return kind ? 128 : 256; }
 
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -210,27 +212,29 @@ __device__ __forceinline__ bool read_item(const AttnArgs &a, int kind, int item,
   return true;
 }
 
-// The parts of a split context are joined by the workgroup that finishes last, in part
-// order whichever it is:  m = max m_p, l = sum l_p e^(m_p - m), o = sum o_p e^(m_p - m) / l.
-// w: LDS of this workgroup, at least 2 x max_parts x R floats.
-template <typename T, int R>
+// The parts of a split context are joined in part order:  m = max m_p, l = sum l_p e^(m_p - m),
+// o = sum o_p e^(m_p - m) / l.
+
+// Few rows: by the workgroup that finishes last, whichever it is.
+// w: LDS of this workgroup, at least 2 x max_parts x kRowsSmall floats.
+template <typename T>
 __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, const Item &it, int head, int row0,
                                            int n, float *w) {
   using V4 = typename Elem<T>::v4;
-  constexpr int kind = R > kRowsSmall;
+  constexpr int R = kRowsSmall;
   __shared__ int last;
   __shared__ float l_sum[R];
   const int tid = threadIdx.x, nt = (int)blockDim.x;
   parts_arrived();
   __syncthreads();
   if (tid == 0) {
-    int *done = a.plan.done[kind] + (int64_t)it.join * a.Hkv + head;
+    int *done = a.plan.done[0] + (int64_t)it.join * a.Hkv + head;
     last = atomicAdd(done, 1) == it.n - 1;
     if (last) *done = 0;  // for the next layer's call
   }
   __syncthreads();
   if (!last) return;
-  const float *ml = a.plan.ml[kind], *o = a.plan.o[kind];
+  const float *ml = a.plan.ml[0], *o = a.plan.o[0];
   const int64_t base = ((int64_t)it.slot * a.Hkv + head) * R, step = (int64_t)a.Hkv * R;
   // maxima and sums of all parts to LDS at once; then a row's weights of the parts, and lse
   float *wl = w + it.n * R;
@@ -253,7 +257,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, con
     }
     l_sum[rr] = l > 0.f || l != l ? 1.f / l : 0.f;
     const int j = (row0 + rr) / a.G, g = row0 + rr - j * a.G;
-    if (a.lse) a.lse[(int64_t)(r.q0 + j) * a.H + head * a.G + g] = log_sum(m, l, a.s2, weight_shift<T>(kind));
+    if (a.lse) a.lse[(int64_t)(r.q0 + j) * a.H + head * a.G + g] = log_sum(m, l, a.s2, weight_shift<T>(0));
   }
   __syncthreads();
   const int quads = a.D / 4;
@@ -271,6 +275,88 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, con
     *(V4 *)out = __builtin_convertvector(acc * l_sum[rr], V4);
   }
 }
+
+// Many rows: by workgroups of the few-row kernel, which is launched after the many-row kernel, past those of its
+// own items: kJoinBlocks of them go round the plan's items, and an item's workgroup takes its share of its tile's rows.
+// One workgroup reads past its L2 at 8 GB/s only, and a part of 128 rows of 128 columns has 64 KB; after the kernel
+// that wrote them every workgroup may read them through its own (40 tokens of 32 heads on 8 on 1000: 48 us where the
+// last workgroup joined, 22 so; 100 on 10,000 twice 111 and 76).  R: rows of a tile.
+constexpr int kJoinBlocks = 512, kJoinRows = 16;
+struct JoinLds {
+  float w[kJoinRows][max_parts(1)], wl[kJoinRows][max_parts(1)], l_sum[kJoinRows];  // weights, sums, 1 / l
+  f32x4 part[256];
+};
+template <typename T>
+__device__ __forceinline__ void join_many(const AttnArgs &a, int R, int block, JoinLds &s) {
+  using V4 = typename Elem<T>::v4;
+  const int tid = threadIdx.x, quads = a.D / 4;
+  const int64_t n_work = (int64_t)min(a.plan.hdr->n_items[1], a.plan.cap_items[1]) * a.Hkv;
+  for (int64_t work = block; work < n_work; work += kJoinBlocks) {
+    const int item = (int)(work / a.Hkv), head = (int)(work - (int64_t)item * a.Hkv);
+    Item it;
+    Rows r;
+    if (!read_item(a, 1, item, it, r) || it.n < 2) continue;
+    const int n_rows = r.nq * a.G, n_rt = (n_rows + R - 1) / R;
+    if (it.tile >= n_rt) continue;
+    const int row0 = (n_rt - 1 - it.tile) * R, n = min(n_rows - row0, R);
+    const int per = (n + it.n - 1) / it.n, first = it.part * per, end = min(first + per, n);
+    const int64_t base = ((int64_t)it.slot * a.Hkv + head) * R, step = (int64_t)a.Hkv * R;
+    const float *ml = a.plan.ml[1], *o = a.plan.o[1];
+    for (int r0 = first; r0 < end; r0 += kJoinRows) {
+      const int m_rows = min(kJoinRows, end - r0);
+      __syncthreads();
+      for (int x = tid; x < m_rows * it.n; x += 256) {
+        const int p = x / m_rows, rr = x - p * m_rows;
+        const float2 y = *(const float2 *)(ml + (base + p * step + r0 + rr) * 2);
+        s.w[rr][p] = y.x;
+        s.wl[rr][p] = y.y;
+      }
+      __syncthreads();
+      for (int x = tid; x < m_rows * 4; x += 256) {  // four lanes a row
+        const int rr = x >> 2;
+        float m = kNegInf, l = 0.f;
+        for (int p = x & 3; p < it.n; p += 4) m = fmaxf(m, s.w[rr][p]);
+        m = fmaxf(m, __shfl_xor(m, 1));
+        m = fmaxf(m, __shfl_xor(m, 2));
+        const float mu = m == kNegInf ? 0.f : m;
+        for (int p = x & 3; p < it.n; p += 4) {
+          const float f = exp2_hw((s.w[rr][p] - mu) * a.s2);
+          s.w[rr][p] = f;
+          l = fmaf(f, s.wl[rr][p], l);
+        }
+        l += __shfl_xor(l, 1);
+        l += __shfl_xor(l, 2);
+        if ((x & 3) == 0) {
+          s.l_sum[rr] = l > 0.f || l != l ? 1.f / l : 0.f;
+          const int row = row0 + r0 + rr, j = row / a.G, g = row - j * a.G;
+          if (a.lse) a.lse[(int64_t)(r.q0 + j) * a.H + head * a.G + g] = log_sum(m, l, a.s2, weight_shift<T>(1));
+        }
+      }
+      __syncthreads();
+      // where there are more threads than groups of four columns, they share a row's parts
+      const int total = m_rows * quads, share = max(256 / total, 1), mine = share > 1 ? tid / total : 0;
+      for (int x = tid - mine * total; x < total; x += 256) {
+        const int rr = x / quads, d4 = x - rr * quads;
+        const float *src = o + (base + r0 + rr) * a.D + d4 * 4;
+        f32x4 acc = {0, 0, 0, 0};
+        if (mine < share) {
+#pragma unroll 8
+          for (int p = mine; p < it.n; p += share) acc += *(const f32x4 *)(src + p * step * a.D) * s.w[rr][p];
+        }
+        if (share > 1) {
+          s.part[tid] = acc;
+          __syncthreads();  // every thread comes here, and once
+          if (mine > 0) break;
+          for (int i = 1; i < share; i++) acc += s.part[i * total + tid];
+        }
+        const int row = row0 + r0 + rr, j = row / a.G, g = row - j * a.G;
+        T *out = (T *)a.out + ((int64_t)(r.q0 + j) * a.H + head * a.G + g) * a.D + d4 * 4;
+        *(V4 *)out = __builtin_convertvector(acc * s.l_sum[rr], V4);
+      }
+    }
+  }
+}
+
 // The order of a matrix phase for the instruction scheduler: NK products with one
 // operand read from LDS each, then NV with two reads each; reads run AHEAD products
 // in front, so that a product's operands have arrived when the unit is free for it.
@@ -715,7 +801,6 @@ __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_
   if (any_bad)
     add_specials<T, PAGED, C8>(a, r, k0, it.seq, it.n > 1 ? it.slot + it.part : -1, R, head, row0, min(n_rows - row0, R),
                            it.lo + (max(all_wg - it.lo, 0) & ~63), hi);
-  if (PAGED && it.n > 1) join_parts<T, R>(a, r, it, head, row0, min(n_rows - row0, R), (float *)lds_k[0]);
 }
 
 }  // namespace

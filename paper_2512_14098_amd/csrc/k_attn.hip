@@ -96,7 +96,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
 #pragma unroll
   for (int k = 0; k < 2; k++) {
     const Split sp = k ? sp1 : sp0;
-    const int least = max(kMinPart, (int)(w[2 + k] * 1.001f) / sp.max_parts + 2);
+    const int least = max(min_part(k), (int)(w[2 + k] * 1.001f) / sp.max_parts + 2);
 #pragma unroll
     for (int c = 0; c < 3; c++) {
       const float even = c == 0 ? 0x1p30f : fminf(w[k] * 1.001f / (float)(sp.n * c) + 1.f, 0x1p30f);
@@ -253,13 +253,18 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
 // 85 us, 6.3 TB/s.  Two workgroups a CU hold 128 KB in flight; a third (168
 // registers, 7 spilled) is 10 % slower.  The matrix unit is busy 4 % of the time,
 // also where one of its 16 rows is used.
-template <typename T, int KS, int DB, int DS>
-__global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) {
+template <typename T, int KS, int DB, int DS, bool JOIN>
+__global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a, int own_blocks, int join_rows) {
   using V8 = typename Elem<T>::v8;
   using V4 = typename Elem<T>::v4;
   constexpr int CH = DS / 8, NV = 32 * CH / 64;
   __shared__ __attribute__((aligned(16))) char lds[4][32 * DS * 2];
+  static_assert(sizeof(JoinLds) <= sizeof(lds), "");
   __shared__ float l_m[4][16], l_l[4][16];
+  if (JOIN && (int)blockIdx.x >= own_blocks) {
+    join_many<T>(a, join_rows, (int)blockIdx.x - own_blocks, *(JoinLds *)lds[0]);
+    return;
+  }
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = (int)(blockIdx.x % (unsigned)a.Hkv), item = (int)(blockIdx.x / (unsigned)a.Hkv);
   Item it;
@@ -431,7 +436,7 @@ __global__ __launch_bounds__(256, DS > 128 ? 1 : 2) void k_attn_few(AttnArgs a) 
   if (any_bad)
     add_specials<T, true>(a, r, 0, it.seq, it.n > 1 ? it.slot + it.part : -1, kRowsSmall, head, row0, min(n_rows - row0, kRowsSmall),
                           it.lo + (max(all - it.lo, 0) & ~31), hi);
-  if (it.n > 1) join_parts<T, kRowsSmall>(a, r, it, head, row0, min(n_rows - row0, kRowsSmall), (float *)lds[0]);
+  if (it.n > 1) join_parts<T>(a, r, it, head, row0, min(n_rows - row0, kRowsSmall), (float *)lds[0]);
 }
 // ------------------------------------------------------------------ host
 cf_status check_heads(int H, int Hkv, int D) {
@@ -487,32 +492,41 @@ void launch_many(const AttnArgs &a, int groups, int64_t blocks, hipStream_t s) {
   else if (a.D <= 128) k_attn_many<T, 8, 4, 128, 2, PAGED, C8><<<g, b, 0, s>>>(a);
   else k_attn_many<T, 16, 8, 256, 1, PAGED, C8><<<g, b, 0, s>>>(a);
 }
-template <typename T>
-void launch_few(const AttnArgs &a, int64_t blocks, hipStream_t s) {
-  const dim3 g((unsigned)blocks), b(256);
-  if (a.D <= 64) k_attn_few<T, 2, 4, 64><<<g, b, 0, s>>>(a);
-  else if (a.D <= 96) k_attn_few<T, 3, 6, 128><<<g, b, 0, s>>>(a);
-  else if (a.D <= 128) k_attn_few<T, 4, 8, 128><<<g, b, 0, s>>>(a);
-  else k_attn_few<T, 8, 16, 256><<<g, b, 0, s>>>(a);
+// JOIN: after the many-row kernel, with workgroups that join its parts; rows: of its tiles.  A decode step's calls
+// have no such workgroups and keep the registers of the kernel without them (8-bit cache, one request of
+// 32767 keys 49 us, 50.4 with them).
+template <typename T, bool JOIN>
+void launch_few(const AttnArgs &a, int64_t blocks, int rows, hipStream_t s) {
+  const dim3 g((unsigned)blocks + (JOIN ? kJoinBlocks : 0)), b(256);
+  const int own = (int)blocks;
+  if (a.D <= 64) k_attn_few<T, 2, 4, 64, JOIN><<<g, b, 0, s>>>(a, own, rows);
+  else if (a.D <= 96) k_attn_few<T, 3, 6, 128, JOIN><<<g, b, 0, s>>>(a, own, rows);
+  else if (a.D <= 128) k_attn_few<T, 4, 8, 128, JOIN><<<g, b, 0, s>>>(a, own, rows);
+  else k_attn_few<T, 8, 16, 256, JOIN><<<g, b, 0, s>>>(a, own, rows);
 }
-template <typename T>
-void launch_few8(const AttnArgs &a, int64_t blocks, hipStream_t s) {
+template <typename T, bool JOIN>
+void launch_few8(const AttnArgs &a, int64_t blocks, int rows, hipStream_t s) {
   const int64_t round = 8 * few8_heads(a.Hkv, a.page_log2);
-  const dim3 g((unsigned)((blocks + round - 1) / round * round)), b(256);
-  if (a.D <= 64) k_attn_few8<T, 2, 4, 64><<<g, b, 0, s>>>(a);
-  else if (a.D <= 96) k_attn_few8<T, 4, 6, 128><<<g, b, 0, s>>>(a);
-  else if (a.D <= 128) k_attn_few8<T, 4, 8, 128><<<g, b, 0, s>>>(a);
-  else k_attn_few8<T, 8, 16, 256><<<g, b, 0, s>>>(a);
+  const int own = (int)((blocks + round - 1) / round * round);
+  const dim3 g((unsigned)own + (JOIN ? kJoinBlocks : 0)), b(256);
+  if (a.D <= 64) k_attn_few8<T, 2, 4, 64, JOIN><<<g, b, 0, s>>>(a, own, rows);
+  else if (a.D <= 96) k_attn_few8<T, 4, 6, 128, JOIN><<<g, b, 0, s>>>(a, own, rows);
+  else if (a.D <= 128) k_attn_few8<T, 4, 8, 128, JOIN><<<g, b, 0, s>>>(a, own, rows);
+  else k_attn_few8<T, 8, 16, 256, JOIN><<<g, b, 0, s>>>(a, own, rows);
 }
 template <typename T>
 void launch_paged(const AttnArgs &a, bool c8, bool few, int groups, hipStream_t s) {
   const int64_t blocks0 = (int64_t)a.plan.cap_items[0] * a.Hkv, blocks1 = (int64_t)a.plan.cap_items[1] * a.Hkv;
-  if (c8) {
-    launch_few8<T>(a, blocks0, s);
-    if (!few) launch_many<T, true, true>(a, groups, blocks1, s);
+  const int rows = kRowsGroup * groups;
+  if (few) {
+    if (c8) launch_few8<T, false>(a, blocks0, 0, s);
+    else launch_few<T, false>(a, blocks0, 0, s);
+  } else if (c8) {
+    launch_many<T, true, true>(a, groups, blocks1, s);
+    launch_few8<T, true>(a, blocks0, rows, s);
   } else {
-    launch_few<T>(a, blocks0, s);
-    if (!few) launch_many<T, true>(a, groups, blocks1, s);
+    launch_many<T, true>(a, groups, blocks1, s);
+    launch_few<T, true>(a, blocks0, rows, s);
   }
 }
 
@@ -532,7 +546,7 @@ static int desc_groups(const cf_attn_desc *d) {
 
 // Workgroups of the kernels that run at a time per key/value head, as the plan counts on
 // them, and what a part costs beside its keys (measured: starting and joining one takes the
-// few-row kernel as long as 64 keys, the many-row kernel as long as 400).
+// few-row kernel as long as 64 keys, the many-row kernel as long as 400; 150 there makes no difference).
 static Split split_of(const cf_attn_desc *d, int kind) {
   const int per_cu = kind ? (desc_groups(d) > 1 || d->head_dim > 128 ? 1 : 2) : (d->head_dim > 128 ? 1 : 2);
   return Split{(256 * per_cu + d->n_kv_heads - 1) / d->n_kv_heads, kind ? 400 : 64, max_parts(kind)};
