@@ -6,7 +6,9 @@ card is the part that depends on context lengths, the attention over the cache, 
 an executor's profile (Sec. 5.1) holds.  This module measures it: requests come from the workload's trace, an executor admits them in batches of the
 batch knob, and each iteration runs the calls that a serving step makes - cf_kv_map for the step,
 cf_kv_write and cf_attn_paged for each layer on one cf_attn_plan, cf_attn_prompt for an encoder's
-batch.  Keys, values and queries are random.  Layers and heads are the caller's: no workload holds
+batch.  With --rope queries and keys are turned by their positions in every layer (cf_rope), with
+--cache8 the caches hold e4m3 codes: cf_kv_write8 or, with both, cf_rope_write8 for each layer, cf_attn_paged8,
+and the hand-over of the prefilled requests to another executor (cf_kv_read8).  Keys, values and queries are random.  Layers and heads are the caller's: no workload holds
 them, so the seconds stand beside the latency model's and are no share of it.
 
 Layers have caches of their own, as many as make one pass over the layers read PASS_BYTES, twice
@@ -15,7 +17,7 @@ layers, small batches would be read from there, which no executor's are (16 requ
 a decode step of 1.35 ms, 1.31 with one cache).  Times are those of the calls in a row: where the kernels
 are shorter than the calls (4 requests: 0.70 ms for 65 of them), the calls'.
 
-    python -m paper_2512_14098_amd.attn_profile --config c1 --batch 64 --layers 32
+    python -m paper_2512_14098_amd.attn_profile --config c1 --batch 64 --layers 32 [--rope] [--cache8]
 """
 import argparse
 
@@ -80,10 +82,12 @@ def encoder_sequences(model, trace, component, seed, requests, device="cuda"):
 
 class PagedExecutor:
     """One executor's paged cache and the attention of its iterations.  tokens: those that a step
-    reads of each layer's cache (all that it holds if not given), for the number of caches."""
+    reads of each layer's cache (all that it holds if not given), for the number of caches.  rope: the base of
+    the rotary frequencies, by which queries and keys are turned (None: not at all).  cache8: e4m3
+    caches, each a triple of codes of keys and of values and exponents."""
 
     def __init__(self, slots, longest, layers, heads, kv_heads, dim, page=16, dtype=torch.bfloat16, device="cuda",
-                 tokens=None):
+                 tokens=None, rope=None, cache8=False):
         self.layers, self.heads, self.kv_heads, self.dim, self.page = layers, heads, kv_heads, dim, page
         rows = -(-longest // page)
         n_pages = slots * rows
@@ -91,25 +95,56 @@ class PagedExecutor:
         self.free = torch.arange(n_pages, dtype=torch.int32, device=device)
         self.head = torch.zeros(1, dtype=torch.int32, device=device)
         shape = (n_pages, kv_heads, page, dim)
-        read = 2 * (n_pages * page if tokens is None else max(int(tokens), 1)) * kv_heads * dim * dtype.itemsize
-        self.caches = [tuple(torch.randn(shape, dtype=dtype, device=device) for _ in range(2))
+        row = 2 * kv_heads * (dim + 1 if cache8 else dim * dtype.itemsize)
+        read = (n_pages * page if tokens is None else max(int(tokens), 1)) * row
+        self.cache8, self.freq = cache8, None
+        if rope is not None:
+            self.freq = torch.from_numpy(float(rope) ** (-np.arange(dim // 2) / (dim // 2))).to(device)
+        self.caches = [self._cache8(shape, device) if cache8 else
+                       tuple(torch.randn(shape, dtype=dtype, device=device) for _ in range(2))
                        for _ in range(max(1, min(layers, -(-PASS_BYTES // read))))]
         self.qkv = torch.empty((0, heads + 2 * kv_heads, dim), dtype=dtype, device=device)
+
+    @staticmethod
+    def _cache8(shape, device):
+        codes = [torch.randint(0, 127, shape, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+                 for _ in range(2)]
+        exps = torch.full((shape[0], shape[1], 2, shape[2]), 120, dtype=torch.uint8, device=device)
+        return codes[0], codes[1], exps
 
     def step(self, ctx_len, new_len, n_tok, max_new):
         """One iteration: returns its attention output (the last layer's) and the status words."""
         if self.qkv.shape[0] < n_tok:
             self.qkv = torch.randn((n_tok,) + tuple(self.qkv.shape[1:]), dtype=self.qkv.dtype, device=self.qkv.device)
         x, h, g = self.qkv[:n_tok], self.heads, self.kv_heads
-        q_start, kv_len, slots, _, head, status = cf.cf_kv_map(ctx_len, new_len, self.table, self.page, self.free,
-                                                               self.head, n_tok)
+        q_start, kv_len, slots, pos, head, status = cf.cf_kv_map(ctx_len, new_len, self.table, self.page, self.free,
+                                                                 self.head, n_tok)
         self.head = head
         plan = cf.cf_attn_plan(q_start, kv_len, n_tok, max_new, h, g, self.dim)
         for layer in range(self.layers):
-            k_cache, v_cache = self.caches[layer % len(self.caches)]
-            cf.cf_kv_write(x[:, h:h + g], x[:, h + g:], k_cache, v_cache, slots)
-            out = cf.cf_attn_paged(plan, x[:, :h], k_cache, v_cache, self.table)
+            cache = self.caches[layer % len(self.caches)]
+            q, k, v = x[:, :h], x[:, h:h + g], x[:, h + g:]
+            if self.cache8:
+                if self.freq is None:
+                    cf.cf_kv_write8(k, v, *cache, slots)
+                else:
+                    q = cf.cf_rope_write8(q, k, v, pos, self.freq, None, *cache, slots)
+                out = cf.cf_attn_paged8(plan, q, *cache, self.table)
+            else:
+                if self.freq is not None:
+                    q, k = cf.cf_rope(q, k, pos, self.freq)
+                cf.cf_kv_write(k, v, *cache, slots)
+                out = cf.cf_attn_paged(plan, q, *cache, self.table)
         return out, status
+
+    def hand_over(self, lens, n_tok):
+        """Every layer's cached tokens of the requests, lens int32 [slots] of them, as packed 16-bit rows: the
+        last layer's keys and values and the starts."""
+        start = torch.zeros(len(lens) + 1, dtype=torch.int32, device=lens.device)
+        torch.cumsum(lens, 0, dtype=torch.int32, out=start[1:])
+        for layer in range(self.layers):
+            k, v = cf.cf_kv_read8(*self.caches[layer % len(self.caches)], self.table, start, n_tok, self.qkv.dtype)
+        return k, v, start
 
 
 def _timed(fn):
@@ -122,10 +157,11 @@ def _timed(fn):
 
 
 def profile(config, component=None, batch=64, layers=32, heads=32, kv_heads=8, dim=128, page=16, decode_steps=4,
-            n_req=1000, seed=0, device="cuda"):
+            n_req=1000, seed=0, device="cuda", rope=None, cache8=False):
     """Attention seconds of one prefill and of decode steps of ``batch`` requests of the
     workload's first LLM (or ``component``), beside the latency model's seconds; for each
-    encoder, the attention of a batch of its inputs."""
+    encoder, the attention of a batch of its inputs.  rope, cache8: as PagedExecutor takes them; an
+    8-bit cache's rows have one more, the hand-over of the prefilled requests."""
     cfg = load_config(config) if isinstance(config, str) else config
     model = cfg["model"]
     desc = cf.model_desc(model)
@@ -138,8 +174,9 @@ def profile(config, component=None, batch=64, layers=32, heads=32, kv_heads=8, d
     n = len(x)
     if n == 0:
         raise cf.CfError("no request of the trace runs " + llm)
+    more = dict(rope=rope, cache8=cache8) if rope is not None or cache8 else {}
     ex = PagedExecutor(n, int(x.max()) + decode_steps + 1, layers, heads, kv_heads, dim, page, device=device,
-                       tokens=int(x.sum()))
+                       tokens=int(x.sum()), **more)
     rows = []
     ctx = torch.zeros(n, dtype=torch.int32, device=device)
     new = torch.as_tensor(x.astype(np.int32)).to(device)
@@ -153,6 +190,11 @@ def profile(config, component=None, batch=64, layers=32, heads=32, kv_heads=8, d
         raise cf.CfError("the cache does not hold the batch")
     rows.append(dict(step="prefill", component=llm, requests=n, tokens=int(x.sum()), attention_s=s,
                      model_s=k0 + k1 * float(x.sum()) + k2 * n))
+    if cache8:
+        run = lambda: ex.hand_over(new, int(x.sum()))
+        _timed(run)
+        rows.append(dict(step="hand over", component=llm, requests=n, tokens=int(x.sum()), attention_s=_timed(run)[1],
+                         model_s=0.0))
     ctx = new.clone()
     for i in range(decode_steps):
         (_, status), s = _timed(lambda: ex.step(ctx, ones, n, 1))
@@ -184,8 +226,11 @@ def main(argv=None):
     p.add_argument("--component")
     for name, value in (("batch", 64), ("layers", 32), ("heads", 32), ("kv-heads", 8), ("dim", 128), ("page", 16)):
         p.add_argument("--" + name, type=int, default=value)
+    p.add_argument("--rope", type=float, nargs="?", const=10000.0, help="turn queries and keys; the frequencies' base")
+    p.add_argument("--cache8", action="store_true", help="e4m3 caches")
     a = p.parse_args(argv)
-    for r in profile(a.config, a.component, a.batch, a.layers, a.heads, a.kv_heads, a.dim, a.page):
+    for r in profile(a.config, a.component, a.batch, a.layers, a.heads, a.kv_heads, a.dim, a.page, rope=a.rope,
+                     cache8=a.cache8):
         print("%-10s %-8s %4d requests %8d tokens  attention %9.3f ms  latency model %9.3f ms"
               % (r["step"], r["component"], r["requests"], r["tokens"], r["attention_s"] * 1e3, r["model_s"] * 1e3))
 
