@@ -97,7 +97,8 @@ __device__ __forceinline__ V8 join8(V4 a, V4 b) {
 struct PlanHdr {
   int32_t n_items[2];  // few-row and many-row kernel
   int32_t part[2];     // keys of a part of a split context
-  int32_t pad[12];
+  int32_t n_split;     // split tiles of the many-row kernel
+  int32_t pad[11];
 };
 struct PlanItem {
   int32_t seq, tile, part, n;  // part of n of the context of a tile of rows
@@ -108,7 +109,9 @@ struct PlanItem {
 struct PlanView {
   PlanHdr *hdr;
   PlanItem *items[2];
-  int32_t *done[2];    // [split tile][key/value head]: parts finished, zero between calls
+  // few rows: [split tile][key/value head], parts finished, zero between calls; many rows: [split tile],
+  // the item of its first part
+  int32_t *done[2];
   float *o[2], *ml[2];  // partial results: [slot][key/value head][row]
   int32_t cap_items[2], cap_slots[2], cap_join[2];
 };

@@ -277,7 +277,7 @@ __device__ __forceinline__ void join_parts(const AttnArgs &a, const Rows &r, con
 }
 
 // Many rows: by workgroups of the few-row kernel, which is launched after the many-row kernel, past those of its
-// own items: kJoinBlocks of them go round the plan's items, and an item's workgroup takes its share of its tile's rows.
+// own items: kJoinBlocks of them share the split tiles and, where those are few, their rows.
 // One workgroup reads past its L2 at 8 GB/s only, and a part of 128 rows of 128 columns has 64 KB; after the kernel
 // that wrote them every workgroup may read them through its own (40 tokens of 32 heads on 8 on 1000: 48 us where the
 // last workgroup joined, 22 so; 100 on 10,000 twice 111 and 76).  R: rows of a tile.
@@ -290,16 +290,20 @@ template <typename T>
 __device__ __forceinline__ void join_many(const AttnArgs &a, int R, int block, JoinLds &s) {
   using V4 = typename Elem<T>::v4;
   const int tid = threadIdx.x, quads = a.D / 4;
-  const int64_t n_work = (int64_t)min(a.plan.hdr->n_items[1], a.plan.cap_items[1]) * a.Hkv;
-  for (int64_t work = block; work < n_work; work += kJoinBlocks) {
-    const int item = (int)(work / a.Hkv), head = (int)(work - (int64_t)item * a.Hkv);
+  const int64_t tiles = (int64_t)clampi(a.plan.hdr->n_split, 0, a.plan.cap_join[1]) * a.Hkv;
+  if (tiles == 0) return;
+  const int shares = clampi((int)(kJoinBlocks / tiles), 1, R / 8);
+  for (int64_t work = block; work < tiles * shares; work += kJoinBlocks) {
+    const int64_t tile = work / shares;
+    const int share_no = (int)(work - tile * shares), split = (int)(tile / a.Hkv), head = (int)(tile - (int64_t)split * a.Hkv);
     Item it;
     Rows r;
-    if (!read_item(a, 1, item, it, r) || it.n < 2) continue;
+    const int item = a.plan.done[1][split];
+    if (item < 0 || !read_item(a, 1, item, it, r) || it.n < 2) continue;
     const int n_rows = r.nq * a.G, n_rt = (n_rows + R - 1) / R;
     if (it.tile >= n_rt) continue;
     const int row0 = (n_rt - 1 - it.tile) * R, n = min(n_rows - row0, R);
-    const int per = (n + it.n - 1) / it.n, first = it.part * per, end = min(first + per, n);
+    const int per = (n + shares - 1) / shares, first = share_no * per, end = min(first + per, n);
     const int64_t base = ((int64_t)it.slot * a.Hkv + head) * R, step = (int64_t)a.Hkv * R;
     const float *ml = a.plan.ml[1], *o = a.plan.o[1];
     for (int r0 = first; r0 < end; r0 += kJoinRows) {

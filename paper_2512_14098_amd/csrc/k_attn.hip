@@ -76,8 +76,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
   if (tid < n_seq) load(tid, tiles0, kind0, keys0);
   const int first_q0 = q0, first_nq = nq, first_nk = nk;
   // the counters of finished parts start at zero
-  for (int k = 0; k < 2; k++)
-    for (int i = tid; i < v.cap_join[k] * Hkv; i += NT) v.done[k][i] = 0;
+  for (int i = tid; i < v.cap_join[0] * Hkv; i += NT) v.done[0][i] = 0;
   float w[4] = {0.f, 0.f, 0.f, 0.f};  // work of either kernel, longest contexts
   for (int i = tid; i < n_seq; i += NT) {
     int tiles = tiles0, kind = kind0, keys = keys0;
@@ -224,6 +223,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
         if (np > 1) {
           it.slot = slots[k] + (int)((uint64_t)b >> 40 & 0xfff) + tile * (int)np;
           it.join = joins[k] + (int)((uint64_t)b >> 52) + tile;
+          if (k == 1 && pi == 0 && it.join < v.cap_join[1]) v.done[1][it.join] = (int)(at[k] + y);
         }
         v.items[k][at[k] + y] = it;
       }
@@ -232,6 +232,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
       joins[k] += (int)((uint64_t)total >> 52);
     }
   }
+  if (tid == 0) v.hdr->n_split = min(joins[1], v.cap_join[1]);
   if (tid < 2) {
     v.hdr->n_items[tid] = (int)min(at[tid], (int64_t)v.cap_items[tid]);
     v.hdr->part[tid] = part[tid];
