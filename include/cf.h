@@ -650,7 +650,7 @@ cf_status cf_attn_prompt(const cf_attn_seqs *a, float scale, void *out_dev, floa
  *
  * Cache: one layer's keys and values, e4m3 codes [n_pages][n_kv_heads][page][head_dim] each, and
  * a byte per row of either, [n_pages][n_kv_heads][2][page], keys' before values': the row's scale is
- * 2^(byte - 127).  Pages and slots as above; head_dim is a multiple of 16, 16..256; pointers
+ * 2^(byte - 127), byte 255 makes it NaN.  Pages and slots as above; head_dim is a multiple of 16, 16..256; pointers
  * are 16-byte aligned.  A row x is written with the smallest scale 2^e, e >= -126, such that
  * max |x| <= 448 * 2^e over its finite elements, and each element as the nearest code to x * 2^-e,
  * ties to even; |x| is cut at 61440 in fp16 and 1.875 * 2^127 in bf16, so that every value held is one of the
@@ -674,8 +674,9 @@ typedef struct cf_rope_desc {
 
 /* Queries [n_tok][n_heads][head_dim] and keys [n_tok][n_kv_heads][head_dim] (none with n_kv_heads 0) turned by
  * their positions into q_out_dev and k_out_dev.  Strides are in elements and multiples of 8.
- * An output may be its input, with the same strides; else outputs and inputs do not overlap.
- * Errors: CF_EINVAL (sizes, alignment, NULL arrays, in place with other strides). */
+ * An output may be its input, with the same strides; else outputs and inputs do not overlap, nor the
+ * rows of an output one another.
+ * Errors: CF_EINVAL (sizes, alignment, NULL arrays, in place with other strides, one output for both). */
 cf_status cf_rope(const cf_rope_desc *r, int32_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                   int32_t dtype, const void *q_dev, int64_t q_tok, int64_t q_head, void *q_out_dev, int64_t qo_tok,
                   int64_t qo_head, const void *k_dev, int64_t k_tok, int64_t k_head, void *k_out_dev, int64_t ko_tok,

@@ -455,6 +455,7 @@ extern "C" cf_status cf_rope(const cf_rope_desc *r, int32_t n_tok, int32_t n_hea
   if (!place_ok(q_dev, q_tok, q_head, q_out_dev, qo_tok, qo_head) ||
       (n_kv_heads > 0 && !place_ok(k_dev, k_tok, k_head, k_out_dev, ko_tok, ko_head)))
     return set_error(CF_EINVAL, "in place with other strides");
+  if (n_kv_heads > 0 && q_out_dev == k_out_dev) return set_error(CF_EINVAL, "q_out_dev is k_out_dev");
   a.q = q_dev; a.q_tok = q_tok; a.q_head = q_head;
   a.q_out = q_out_dev; a.qo_tok = qo_tok; a.qo_head = qo_head;
   a.k = k_dev; a.k_tok = k_tok; a.k_head = k_head;
@@ -513,7 +514,7 @@ extern "C" cf_status cf_kv_read8(const cf_kv_cache8 *cache, const int32_t *table
   using namespace cf;
   const cf_status st = check_cache8(cache);
   if (st != CF_OK) return st;
-  if (n_seq < 1 || n_tok < 0 || max_pages < 1)
+  if (n_seq < 1 || n_seq > 1 << 30 || n_tok < 0 || max_pages < 1)
     return set_error(CF_EINVAL, "n_seq %d, n_tok %d, max_pages %d", n_seq, n_tok, max_pages);
   if (n_tok == 0) return CF_OK;
   if (!table_dev || !k_start_dev || !k_out_dev || !v_out_dev) return set_error(CF_EINVAL, "NULL array");

@@ -88,6 +88,25 @@ def test_rope_in_place(cf, n):
     assert torch.equal(x[:, :8], q) and torch.equal(x[:, 8:10], k) and torch.equal(x[:, 10:], rest)
 
 
+def test_rope_in_place_refuses(cf):
+    """Tensors that would have to be copied first, rows that overlap, one tensor for both."""
+    rng = np.random.default_rng(0)
+    t = _dev(*_turning(rng, 6, 64, 1))
+    x = _rand(0, (6, 3, 65), "bf16")
+    for q in (x[:, :, 1:], x[:, :, :64], _rand(0, (1, 3, 64), "bf16").expand(6, 3, 64),
+              _rand(0, (6, 1, 64), "bf16").expand(6, 3, 64)):
+        with pytest.raises(cf.CfError, match="in place"):
+            cf.cf_rope(q, None, *t, in_place=True)
+    y = _rand(0, (6, 3, 64), "bf16")
+    with pytest.raises(cf.CfError, match="k_out_dev"):
+        cf.cf_rope(y, y, *t, in_place=True)
+    a, b = cf.cf_rope(y, y, *t)  # not in place: twice the same
+    assert torch.equal(a, b)
+    # a broadcast tensor is read as it is
+    z = _rand(0, (1, 3, 64), "bf16").expand(6, 3, 64)
+    assert torch.equal(cf.cf_rope(z, None, *t), cf.cf_rope(z.contiguous(), None, *t))
+
+
 def test_rope_far_positions_and_missing_axes(cf):
     """Positions up to 2^31 - 1 and below 0; axes that do not exist turn nothing."""
     pos = np.array([[2 ** 31 - 1, -2 ** 31, 0, 10 ** 9, -1], [1, 2, 3, 4, 5]], np.int32)

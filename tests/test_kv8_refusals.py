@@ -85,7 +85,8 @@ def test_rotary_description(cf, bad):
     dict(n=-1), dict(heads=0), dict(heads=65536), dict(kv=-1), dict(kv=65536), dict(dim=0), dict(dim=68), dict(dim=264),
     dict(dtype=3), dict(q=(None, 512, 64)), dict(qo=(None, 512, 64)), dict(k=(None, 512, 64)), dict(ko=(None, 512, 64)),
     dict(q=(PTR + 8, 512, 64)), dict(q=(PTR, 508, 64)), dict(qo=(PTR, 512, 68)), dict(k=(PTR + 2, 512, 64)),
-    dict(ko=(PTR, 4, 64)), dict(qo=(PTR, 256, 64)), dict(ko=(PTR * 3, 512, 72))])
+    dict(ko=(PTR, 4, 64)), dict(qo=(PTR, 256, 64)), dict(ko=(PTR * 3, 512, 72)),
+    dict(ko=(PTR * 2, 128, 64))])
 def test_rope(cf, bad):
     assert _call_rope(cf, C.byref(_rope(cf)), **bad) == EINVAL
 
@@ -113,7 +114,7 @@ def test_rope_write(cf, bad):
     assert _call_both(cf, C.byref(_rope(cf)), C.byref(_cache(cf)), **bad) == EINVAL
 
 
-@pytest.mark.parametrize("bad", [dict(table=None), dict(most=0), dict(n_seq=0), dict(start=None), dict(n_tok=-1),
+@pytest.mark.parametrize("bad", [dict(table=None), dict(most=0), dict(n_seq=0), dict(n_seq=(1 << 30) + 1), dict(start=None), dict(n_tok=-1),
                                  dict(k=None), dict(v=None), dict(k=PTR + 8), dict(v=PTR + 4)])
 def test_read(cf, bad):
     assert _call_read(cf, C.byref(_cache(cf)), **bad) == EINVAL
