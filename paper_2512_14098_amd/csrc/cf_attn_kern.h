@@ -414,6 +414,9 @@ __device__ __forceinline__ void matrix_order() {
 // wave's state does not fit the registers (32 of them spilled, 55 over a cache): one
 // causal sequence of 4096 tokens, 16 heads of 256, 241 us, 0.57 PFLOP/s; two chunks of
 // 1000 tokens on 24001, 32 heads on 8, 3.4 ms, 0.48 PFLOP/s.  136 to 248 columns take as long.
+// C8, an 8-bit cache: codes are widened between registers and LDS, half the bytes are loaded and staged.
+// Lanes hold the addresses of 16 keys' codes and exponents; worked out by the scalar unit at each load from a row number
+// they cost a third (two chunks of 1000 on 24001, 32 heads on 8: 925 us against 719; the 16-bit cache 746).
 template <typename T, int KS, int DB, int DS, int NG, bool PAGED, bool C8 = false>
 __global__ __launch_bounds__(256 * NG, DS == 64 ? 3 : DS == 128 ? 2 : 1) void k_attn_many(AttnArgs a) {
   using V8 = typename Elem<T>::v8;

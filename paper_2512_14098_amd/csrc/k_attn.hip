@@ -50,7 +50,7 @@ constexpr int kClasses = 18;  // of requests, by the length of their parts
 // One workgroup.  Pass 1 sums the work of either kernel, (row tiles) x (keys), and the
 // parts that each candidate length gives; pass 2 takes NT requests at a time, places their
 // items by a scan and writes them, a thread per item.  Bound by the latency of its few
-// steps (16 to 256 requests: 6 us; with 64-bit divisions and a scan for each count 17), so that 256 threads do better than 1024 as long as
+// steps (16 to 256 requests: 7 us; with 64-bit divisions and a scan for each count 17), so that 256 threads do better than 1024 as long as
 // one step takes all requests.
 template <int NT>
 __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_start, const int32_t *kv_len, int n_seq,
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
 // one is worked on.  The waves' results are joined at the end.
 //
 // Bound by memory: 256 requests of 1767 keys on average (32 heads on 8, 128
-// columns, bf16, pages of 16) 287 us, 6.5 TB/s of cache (a kernel that only reads
+// columns, bf16, pages of 16) 280 us, 6.6 TB/s of cache (a kernel that only reads
 // reaches 6.3 with ordinary loads); one request of 32767 keys on 32 key/value heads
 // 85 us, 6.3 TB/s.  Two workgroups a CU hold 128 KB in flight; a third (168
 // registers, 7 spilled) is 10 % slower.  The matrix unit is busy 4 % of the time,
