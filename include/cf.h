@@ -689,8 +689,9 @@ cf_status cf_kv_write8(const cf_kv_cache8 *cache, int32_t n_tok, const void *k_d
                        const void *v_dev, int64_t v_tok, int64_t v_head, const int64_t *slot_dev, void *stream);
 
 /* Both in one launch: queries turned into q_out_dev, keys turned and written, values
- * written, to the bit what cf_rope and cf_kv_write8 on its keys give.
- * Errors: those of the two. */
+ * written, to the bit what cf_rope and cf_kv_write8 on its keys give.  q_out_dev shares no element with
+ * k_dev or v_dev (it may lie between their rows, as a part of one projection's output).
+ * Errors: those of the two; CF_EINVAL (q_out_dev shares elements with k_dev or v_dev). */
 cf_status cf_rope_write8(const cf_rope_desc *r, const cf_kv_cache8 *cache, int32_t n_tok, int32_t n_heads,
                          const void *q_dev, int64_t q_tok, int64_t q_head, void *q_out_dev, int64_t qo_tok,
                          int64_t qo_head, const void *k_dev, int64_t k_tok, int64_t k_head, const void *v_dev,

@@ -925,7 +925,8 @@ def cf_kv_write8(k, v, k_cache, v_cache, exps, slots):
 
 def cf_rope_write8(q, k, v, pos, freq, axis, k_cache, v_cache, exps, slots, interleaved=False, in_place=False):
     """cf_rope of q and k and cf_kv_write8 of the turned keys and the values in one launch.
-    Returns the turned queries, in a new tensor or with in_place in q; k is left as it is."""
+    Returns the turned queries, in a new tensor or with in_place in q, which then shares no
+    memory with k and v; k is left as it is."""
     c = _kv_cache8(k_cache, v_cache, exps, q.dtype)
     x = _rows(q, "q", None, c.head_dim)
     k, v = _new_rows(c, k, v, q.dtype)

@@ -16,6 +16,7 @@
 // largest power of two first, so that a value held is always one of the element
 // type: without that, fp16 values from 63488 on would be held as 65536.
 #include "cf_attn.h"
+#include "cf_overlap.h"
 
 namespace cf {
 bool page_ok(int page);
@@ -501,6 +502,11 @@ extern "C" cf_status cf_rope_write8(const cf_rope_desc *r, const cf_kv_cache8 *c
     return set_error(CF_EINVAL, "queries are not 16-byte aligned");
   if (!place_ok(q_dev, q_tok, q_head, q_out_dev, qo_tok, qo_head))
     return set_error(CF_EINVAL, "in place with other strides");
+  // a token's queries are written before its keys and values are read
+  const RowSet qo{q_out_dev, n_tok, n_heads, qo_tok, qo_head, a.D};
+  if (rows_meet(qo, RowSet{k_dev, n_tok, a.Hk, k_tok, k_head, a.D}) ||
+      rows_meet(qo, RowSet{v_dev, n_tok, a.Hk, v_tok, v_head, a.D}))
+    return set_error(CF_EINVAL, "q_out_dev shares elements with k_dev or v_dev");
   a.q = q_dev; a.q_tok = q_tok; a.q_head = q_head;
   a.q_out = q_out_dev; a.qo_tok = qo_tok; a.qo_head = qo_head;
   a.n_tok = n_tok; a.Hq = n_heads;

@@ -1,0 +1,56 @@
+"""In-place calls on parts of one tensor: refused where rows share elements, else as out of place."""
+import numpy as np
+import pytest
+
+from tests.test_gpu_kv8 import _cache, _cells, _dev, _rand, _turning
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def cf():
+    from paper_2512_14098_amd import cf as _cf
+    return _cf
+
+
+def test_rope_write8_in_place_refuses_shared_keys_and_values(cf):
+    rng = np.random.default_rng(0)
+    t = _dev(*_turning(rng, 6, 64, 1))
+    x = _rand(0, (6, 12, 64), "bf16")
+    before = x.clone()
+    c = _cache(2, 4, 16, 64)
+    cells = _cells(*c)
+    slots = torch.arange(6).cuda()
+    y, z = x[:, :4], x[:, 8:]
+    for q, k, v in ((y, y, z), (y, z, y), (x[:, :8], x[:, 4:8], z), (x[:, 3:8], z, x[:, :4]), (y, y[2:3].expand(6, 4, 64), z)):
+        with pytest.raises(cf.CfError, match="shares elements"):
+            cf.cf_rope_write8(q, k, v, *t, *c, slots, in_place=True)
+    assert torch.equal(x, before)
+    for a, b in zip(cells, _cells(*c)):
+        assert np.array_equal(a, b)
+    # not in place, the keys may be the queries
+    want = cf.cf_rope(y, None, *t)
+    assert torch.equal(cf.cf_rope_write8(y, y, z, *t, *c, slots), want) and torch.equal(x, before)
+    # keys of one token for all between the queries' rows
+    cf.cf_rope_write8(y, z[1:2].expand(6, 4, 64), z, *t, *c, slots, in_place=True)
+    assert torch.equal(y, want) and torch.equal(x[:, 4:], before[:, 4:])
+
+
+@pytest.mark.parametrize("n", [1, 7, 1600])
+def test_rope_write8_in_place_between_keys_and_values(cf, n):
+    """Parts of a fused projection by head, [token][head][3][dim]: the ranges meet, the rows do not."""
+    rng = np.random.default_rng(n)
+    t = _dev(*_turning(rng, n, 64, 1))
+    x = _rand(1, (n, 5, 3, 64), "fp16")
+    before = x.clone()
+    pages = -(-n // 16)
+    a, b = _cache(pages, 5, 16, 64), _cache(pages, 5, 16, 64)
+    slots = torch.as_tensor(rng.permutation(16 * pages)[:n]).cuda()
+    want = cf.cf_rope_write8(x[:, :, 0], x[:, :, 1], x[:, :, 2], *t, *a, slots)
+    q = x[:, :, 0]
+    assert cf.cf_rope_write8(q, x[:, :, 1], x[:, :, 2], *t, *b, slots, in_place=True) is q
+    assert torch.equal(x[:, :, 0], want) and torch.equal(x[:, :, 1:], before[:, :, 1:])
+    for p, r in zip(_cells(*a), _cells(*b)):
+        assert np.array_equal(p, r)

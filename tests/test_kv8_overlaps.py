@@ -1,0 +1,82 @@
+"""Calls whose outputs share elements with what they read, refused on the host (no GPU needed)."""
+import ctypes as C
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from tests.test_kv8_refusals import EINVAL, PTR, ROOT, _cache, _call_both, _rope, cf, pytestmark  # noqa: F401
+
+CSRC = os.path.join(ROOT, "paper_2512_14098_amd", "csrc")
+
+
+# ------------------------------------------------------------------ the test itself, against sets of elements
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    d = tmp_path_factory.mktemp("overlap")
+    (d / "o.cpp").write_text("""
+#include "cf_overlap.h"
+extern "C" int meet(int64_t a, int64_t b, int64_t n, int64_t ha, int64_t hb, int64_t ta, int64_t tb, int64_t sa,
+                    int64_t sb, int64_t d) {
+  return cf::rows_meet(cf::RowSet{(void *)a, n, ha, ta, sa, d}, cf::RowSet{(void *)b, n, hb, tb, sb, d});
+}
+""")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", CSRC, str(d / "o.cpp"), "-o", str(d / "o.so")])
+    lib = C.CDLL(str(d / "o.so"))
+    lib.meet.argtypes = [C.c_int64] * 10
+    return lib
+
+
+def _elements(p, n, heads, tok, head, d):
+    rows = (p // 2 + np.arange(n)[:, None] * tok + np.arange(heads) * head).ravel()
+    return {int(r) + i for r in rows for i in range(d)}
+
+
+def test_rows_meet(host):
+    """Against sets of elements, strides of either sign, equal and not."""
+    rng = np.random.default_rng(0)
+    seen = {False: 0, True: 0}
+    for _ in range(8000):
+        n, ha, hb, d = (int(x) for x in (rng.integers(1, 5), rng.integers(1, 5), rng.integers(1, 5), 8 * rng.integers(1, 4)))
+        ta, tb, sa, sb = (int(x) * 8 for x in rng.integers(-12, 13, 4))
+        if rng.random() < 0.5:
+            tb = ta
+        if rng.random() < 0.2:
+            ta, tb = [(0, tb), (ta, 0)][rng.integers(2)]
+        if rng.random() < 0.5:
+            sb = sa
+        a = 1 << 20
+        b = a + 16 * int(rng.integers(-40, 41))
+        share = bool(_elements(a, n, ha, ta, sa, d) & _elements(b, n, hb, tb, sb, d))
+        assert bool(host.meet(a, b, n, ha, hb, ta, tb, sa, sb, d)) == share, (n, ha, hb, ta, tb, sa, sb, d, b - a)
+        seen[share] += 1
+    assert min(seen.values()) > 500
+
+
+def test_rows_meet_far(host):
+    """Parts of one large projection's output; strides that reach past memory; more heads than are compared."""
+    q, k, tok = 1 << 30, (1 << 30) + 2 * 32 * 128, 48 * 128
+    assert not host.meet(q, k, 1 << 24, 32, 8, tok, tok, 128, 128, 128)
+    assert host.meet(q, k - 16, 1 << 24, 32, 8, tok, tok, 128, 128, 128)
+    assert host.meet(q, k, 2, 33, 8, tok, tok, 128, 128, 128)
+    assert not host.meet(q, q + 256, 1 << 20, 32, 32, 32 * 384, 32 * 384, 384, 384, 128)  # [token][head][3][128]
+    assert host.meet(q, 1 << 40, 1 << 30, 1, 1, 1 << 40, 8, 8, 8, 8)
+    assert host.meet(q, q + 16, 2, 65535, 65535, 1 << 30, 1 << 30, 16, 24, 8)
+    assert not host.meet(q, 1 << 40, 2, 65535, 65535, 0, 0, 16, 24, 8)
+
+
+# ------------------------------------------------------------------ calls
+X = PTR * 2
+
+
+@pytest.mark.parametrize("args", [
+    dict(q=(X, 512, 64), qo=(X, 512, 64), k=(X, 512, 64)),  # in place, the keys are the queries
+    dict(q=(X, 512, 64), qo=(X, 512, 64), v=(X, 512, 64)),
+    dict(q=(X, 512, 64), qo=(X, 512, 64), k=(X + 3 * 128, 512, 64)),  # the last query head is the first key head
+    dict(q=(X, 512, 64), qo=(X, 512, 64), v=(X + 7 * 128, 512, 64)),  # the second value head is the next token's query
+    dict(qo=(X, 256, 64), k=(X + 512, 0, 64)),  # keys of one token for all, inside the output
+    dict(qo=(X, 256, 64), v=(X + 1024, 512, 64)),  # another token stride
+    dict(qo=(PTR + 16, 256, 64))])
+def test_rope_write8_output_over_keys_or_values(cf, args):
+    assert _call_both(cf, C.byref(_rope(cf)), C.byref(_cache(cf)), **args) == EINVAL
