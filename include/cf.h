@@ -674,9 +674,9 @@ typedef struct cf_rope_desc {
 
 /* Queries [n_tok][n_heads][head_dim] and keys [n_tok][n_kv_heads][head_dim] (none with n_kv_heads 0) turned by
  * their positions into q_out_dev and k_out_dev.  Strides are in elements and multiples of 8.
- * An output may be its input, with the same strides; else outputs and inputs do not overlap, nor the
- * rows of an output one another.
- * Errors: CF_EINVAL (sizes, alignment, NULL arrays, in place with other strides, one output for both). */
+ * An output may be its input, with the same strides; else it shares no element with either input or the other
+ * output (rows may lie between each other's, as parts of one projection's output), nor its rows with one another.
+ * Errors: CF_EINVAL (sizes, alignment, NULL arrays, in place with other strides, an output that shares elements). */
 cf_status cf_rope(const cf_rope_desc *r, int32_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                   int32_t dtype, const void *q_dev, int64_t q_tok, int64_t q_head, void *q_out_dev, int64_t qo_tok,
                   int64_t qo_head, const void *k_dev, int64_t k_tok, int64_t k_head, void *k_out_dev, int64_t ko_tok,

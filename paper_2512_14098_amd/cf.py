@@ -870,7 +870,7 @@ def cf_rope(q, k, pos, freq, axis=None, interleaved=False, inverse=False, in_pla
     freq float64 [pairs], radians a position, axis int32 [pairs] (the axis of each pair; axis 0
     if None).  Pairs are columns (i, pairs + i), or (2i, 2i + 1) with interleaved; columns past the
     pairs pass.  inverse turns back, which is the gradient's turn.  Returns (q, k) in new tensors, or with
-    in_place in the same; k may be None, and q alone is returned."""
+    in_place in the same, which then share no memory; k may be None, and q alone is returned."""
     x = _rows(q, "q")
     n, heads, dim = x.shape
     y = None if k is None else _rows(k, "k", None, dim, x.dtype)

@@ -402,6 +402,8 @@ bool rows_ok(const void *p, int64_t tok, int64_t head) { return !((uintptr_t)p &
 bool place_ok(const void *in, int64_t tok, int64_t head, const void *out, int64_t otok, int64_t ohead) {
   return in != out || (tok == otok && head == ohead);
 }
+// An output beside its input shares no element with it.
+bool beside_ok(const RowSet &in, const RowSet &out) { return in.p == out.p || !rows_meet(out, in); }
 
 cf_status take_write(const cf_kv_cache8 *c, const void *k, int64_t k_tok, int64_t k_head, const void *v, int64_t v_tok,
                      int64_t v_head, const int64_t *slot, TurnArgs *a) {
@@ -457,6 +459,12 @@ extern "C" cf_status cf_rope(const cf_rope_desc *r, int32_t n_tok, int32_t n_hea
       (n_kv_heads > 0 && !place_ok(k_dev, k_tok, k_head, k_out_dev, ko_tok, ko_head)))
     return set_error(CF_EINVAL, "in place with other strides");
   if (n_kv_heads > 0 && q_out_dev == k_out_dev) return set_error(CF_EINVAL, "q_out_dev is k_out_dev");
+  // rows are turned in any order
+  const RowSet q{q_dev, n_tok, n_heads, q_tok, q_head, head_dim}, qo{q_out_dev, n_tok, n_heads, qo_tok, qo_head, head_dim};
+  const RowSet k{k_dev, n_tok, n_kv_heads, k_tok, k_head, head_dim}, ko{k_out_dev, n_tok, n_kv_heads, ko_tok, ko_head, head_dim};
+  if (!beside_ok(q, qo) || !beside_ok(k, ko)) return set_error(CF_EINVAL, "an output shares elements with its input");
+  if (rows_meet(qo, k) || rows_meet(qo, ko) || rows_meet(ko, q))
+    return set_error(CF_EINVAL, "q_out_dev shares elements with the keys, or k_out_dev with the queries");
   a.q = q_dev; a.q_tok = q_tok; a.q_head = q_head;
   a.q_out = q_out_dev; a.qo_tok = qo_tok; a.qo_head = qo_head;
   a.k = k_dev; a.k_tok = k_tok; a.k_head = k_head;
@@ -504,6 +512,8 @@ extern "C" cf_status cf_rope_write8(const cf_rope_desc *r, const cf_kv_cache8 *c
     return set_error(CF_EINVAL, "in place with other strides");
   // a token's queries are written before its keys and values are read
   const RowSet qo{q_out_dev, n_tok, n_heads, qo_tok, qo_head, a.D};
+  if (!beside_ok(RowSet{q_dev, n_tok, n_heads, q_tok, q_head, a.D}, qo))
+    return set_error(CF_EINVAL, "an output shares elements with its input");
   if (rows_meet(qo, RowSet{k_dev, n_tok, a.Hk, k_tok, k_head, a.D}) ||
       rows_meet(qo, RowSet{v_dev, n_tok, a.Hk, v_tok, v_head, a.D}))
     return set_error(CF_EINVAL, "q_out_dev shares elements with k_dev or v_dev");

@@ -54,3 +54,32 @@ def test_rope_write8_in_place_between_keys_and_values(cf, n):
     assert torch.equal(x[:, :, 0], want) and torch.equal(x[:, :, 1:], before[:, :, 1:])
     for p, r in zip(_cells(*a), _cells(*b)):
         assert np.array_equal(p, r)
+
+
+def test_rope_in_place_refuses_overlapping_queries_and_keys(cf):
+    rng = np.random.default_rng(1)
+    t = _dev(*_turning(rng, 5, 64, 1))
+    x = _rand(2, (5, 12, 64), "bf16")
+    before = x.clone()
+    for q, k in ((x[:, :8], x[:, 4:10]), (x[:, 4:], x[:, :5]), (x[:, 3:4], x[:, 3:4]), (x[:, ::2], x[:, 2:6:3])):
+        with pytest.raises(cf.CfError, match="q_out_dev"):
+            cf.cf_rope(q, k, *t, in_place=True)
+    assert torch.equal(x, before)
+
+
+@pytest.mark.parametrize("n", [1, 3, 1700])
+def test_rope_in_place_rows_between_rows(cf, n):
+    """Parts of one tensor that share nothing: by head, by every other head, by every other token."""
+    rng = np.random.default_rng(n)
+    t = _dev(*_turning(rng, n, 32, 1))
+    x = _rand(3, (2 * n, 6, 3, 32), "bf16")
+    for part in (lambda y: (y[:n, :, 0], y[:n, :, 2]), lambda y: (y[:n, ::2, 1], y[:n, 1::2, 1]),
+                 lambda y: (y[::2, :, 0], y[1::2, :, 0]), lambda y: (y[:n, :, 1], y[n:, :2, 1])):
+        y = x.clone()
+        q, k = part(y)
+        qo, ko = cf.cf_rope(*part(x), *t)
+        want = x.clone()
+        for p, o in zip(part(want), (qo, ko)):
+            p.copy_(o)
+        a, b = cf.cf_rope(q, k, *t, in_place=True)
+        assert a is q and b is k and torch.equal(y, want)

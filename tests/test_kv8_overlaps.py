@@ -6,7 +6,7 @@ import subprocess
 import numpy as np
 import pytest
 
-from tests.test_kv8_refusals import EINVAL, PTR, ROOT, _cache, _call_both, _rope, cf, pytestmark  # noqa: F401
+from tests.test_kv8_refusals import EINVAL, PTR, ROOT, _cache, _call_both, _call_rope, _rope, cf, pytestmark  # noqa: F401
 
 CSRC = os.path.join(ROOT, "paper_2512_14098_amd", "csrc")
 
@@ -80,3 +80,22 @@ X = PTR * 2
     dict(qo=(PTR + 16, 256, 64))])
 def test_rope_write8_output_over_keys_or_values(cf, args):
     assert _call_both(cf, C.byref(_rope(cf)), C.byref(_cache(cf)), **args) == EINVAL
+
+
+@pytest.mark.parametrize("args", [
+    dict(q=(X, 512, 64), qo=(X, 512, 64), k=(X, 512, 64)),  # queries in place, the keys are the queries
+    dict(q=(X, 512, 64), k=(X, 512, 64), ko=(X, 512, 64), qo=(PTR * 3, 256, 64)),  # and the other way round
+    dict(q=(X, 512, 64), qo=(X, 512, 64), k=(X + 3 * 128, 512, 64), ko=(X + 3 * 128, 512, 64)),  # shifted by heads
+    dict(q=(X, 512, 64), k=(X + 7 * 128, 512, 64), qo=(PTR * 3, 256, 64), ko=(X + 7 * 128, 512, 64)),
+    dict(qo=(X, 512, 64), ko=(X + 128, 512, 64)),  # outputs over each other
+    dict(qo=(X, 512, 64), ko=(X + 2048, 128, 64)),
+    dict(q=(X, 512, 64), qo=(X + 128, 512, 64)),  # an output a head or a token behind its input
+    dict(q=(X, 512, 64), qo=(X - 1024, 512, 64)),
+    dict(k=(X, 512, 64), ko=(X + 64, 512, 64), qo=(PTR * 5, 256, 64))])
+def test_rope_outputs_over_other_tensors(cf, args):
+    assert _call_rope(cf, C.byref(_rope(cf)), **args) == EINVAL
+
+
+@pytest.mark.parametrize("qo", [(X + 128, 512, 64), (X - 1024, 512, 64), (X + 16, 512, 64)])
+def test_rope_write8_output_beside_its_input(cf, qo):
+    assert _call_both(cf, C.byref(_rope(cf)), C.byref(_cache(cf)), q=(X, 512, 64), qo=qo) == EINVAL
