@@ -858,10 +858,6 @@ def _turned(x, given, in_place, what):
         return torch.empty_like(x, memory_format=torch.contiguous_format)
     if x is not given:
         raise CfError("%s: in place needs rows packed within a head, 16-byte aligned, strides multiples of 8" % what)
-    n, h, d = x.shape
-    s0, s1, _ = x.stride()
-    if (n > 1 and s0 < d) or (h > 1 and s1 < d) or (n > 1 and h > 1 and s0 == s1):
-        raise CfError("%s: in place in rows that overlap" % what)
     return x
 
 

@@ -81,4 +81,22 @@ inline bool rows_meet(RowSet a, RowSet b) {
   return false;
 }
 
+// Whether two rows of a share an element.
+inline bool rows_overlap(const RowSet &a) {
+  if (a.n < 1 || a.heads < 1) return false;
+  int64_t lo, hi;
+  if (!overlap::span(a, lo, hi)) return true;
+  const int64_t tok = a.tok < 0 ? -a.tok : a.tok, head = a.head < 0 ? -a.head : a.head;
+  if (a.heads == 1) return a.n > 1 && tok < a.d;
+  if (a.n == 1) return head < a.d;
+  if (tok < a.d || head < a.d) return true;
+  if (tok >= head * (a.heads - 1) + a.d || head >= tok * (a.n - 1) + a.d) return false;  // one inside the other
+  // rows g numbers apart along the shorter side, at any distance along the other
+  const bool by_head = a.heads <= a.n;
+  const int64_t m = by_head ? a.heads : a.n, sm = by_head ? a.head : a.tok;
+  for (int64_t g = 1; g < m; g++)
+    if (overlap::near(g * sm, by_head ? a.tok : a.head, by_head ? a.n : a.heads, a.d)) return true;
+  return false;
+}
+
 }  // namespace cf

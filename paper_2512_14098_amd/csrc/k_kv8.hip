@@ -462,6 +462,7 @@ extern "C" cf_status cf_rope(const cf_rope_desc *r, int32_t n_tok, int32_t n_hea
   // rows are turned in any order
   const RowSet q{q_dev, n_tok, n_heads, q_tok, q_head, head_dim}, qo{q_out_dev, n_tok, n_heads, qo_tok, qo_head, head_dim};
   const RowSet k{k_dev, n_tok, n_kv_heads, k_tok, k_head, head_dim}, ko{k_out_dev, n_tok, n_kv_heads, ko_tok, ko_head, head_dim};
+  if (rows_overlap(qo) || rows_overlap(ko)) return set_error(CF_EINVAL, "rows of an output overlap, in place or not");
   if (!beside_ok(q, qo) || !beside_ok(k, ko)) return set_error(CF_EINVAL, "an output shares elements with its input");
   if (rows_meet(qo, k) || rows_meet(qo, ko) || rows_meet(ko, q))
     return set_error(CF_EINVAL, "q_out_dev shares elements with the keys, or k_out_dev with the queries");
@@ -512,6 +513,7 @@ extern "C" cf_status cf_rope_write8(const cf_rope_desc *r, const cf_kv_cache8 *c
     return set_error(CF_EINVAL, "in place with other strides");
   // a token's queries are written before its keys and values are read
   const RowSet qo{q_out_dev, n_tok, n_heads, qo_tok, qo_head, a.D};
+  if (rows_overlap(qo)) return set_error(CF_EINVAL, "rows of an output overlap, in place or not");
   if (!beside_ok(RowSet{q_dev, n_tok, n_heads, q_tok, q_head, a.D}, qo))
     return set_error(CF_EINVAL, "an output shares elements with its input");
   if (rows_meet(qo, RowSet{k_dev, n_tok, a.Hk, k_tok, k_head, a.D}) ||

@@ -83,3 +83,21 @@ def test_rope_in_place_rows_between_rows(cf, n):
             p.copy_(o)
         a, b = cf.cf_rope(q, k, *t, in_place=True)
         assert a is q and b is k and torch.equal(y, want)
+
+
+def test_rope_in_place_refuses_rows_over_one_another(cf):
+    """Sliding windows and rows of other tokens' heads; [head][token][dim] and every other row are not such."""
+    rng = np.random.default_rng(2)
+    t = _dev(*_turning(rng, 3, 64, 1))
+    base = _rand(4, (4096,), "bf16")
+    before = base.clone()
+    for size, strides in (((3, 4, 64), (128, 64, 1)), ((3, 3, 64), (64, 128, 1)), ((3, 1, 64), (32, 64, 1)),
+                          ((3, 3, 64), (192, 96, 1))):
+        with pytest.raises(cf.CfError, match="in place"):
+            cf.cf_rope(base.as_strided(size, strides), None, *t, in_place=True)
+    assert torch.equal(base, before)
+    for size, strides in (((3, 4, 64), (64, 192, 1)), ((3, 4, 64), (512, 128, 1)), ((3, 2, 64), (128, 192, 1))):
+        base.copy_(before)
+        q = base.as_strided(size, strides)
+        want = cf.cf_rope(q, None, *t)
+        assert cf.cf_rope(q, None, *t, in_place=True) is q and torch.equal(q, want)

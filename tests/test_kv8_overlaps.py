@@ -21,10 +21,13 @@ extern "C" int meet(int64_t a, int64_t b, int64_t n, int64_t ha, int64_t hb, int
                     int64_t sb, int64_t d) {
   return cf::rows_meet(cf::RowSet{(void *)a, n, ha, ta, sa, d}, cf::RowSet{(void *)b, n, hb, tb, sb, d});
 }
+extern "C" int self(int64_t a, int64_t n, int64_t h, int64_t t, int64_t s, int64_t d) {
+  return cf::rows_overlap(cf::RowSet{(void *)a, n, h, t, s, d});
+}
 """)
     subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", CSRC, str(d / "o.cpp"), "-o", str(d / "o.so")])
     lib = C.CDLL(str(d / "o.so"))
-    lib.meet.argtypes = [C.c_int64] * 10
+    lib.meet.argtypes, lib.self.argtypes = [C.c_int64] * 10, [C.c_int64] * 6
     return lib
 
 
@@ -66,6 +69,22 @@ def test_rows_meet_far(host):
     assert not host.meet(q, 1 << 40, 2, 65535, 65535, 0, 0, 16, 24, 8)
 
 
+def test_rows_overlap(host):
+    """Of one tensor: against sets of elements, and large ones."""
+    rng = np.random.default_rng(1)
+    seen = {False: 0, True: 0}
+    for _ in range(8000):
+        n, h, d = (int(x) for x in (rng.integers(1, 6), rng.integers(1, 6), 8 * rng.integers(1, 4)))
+        tok, head = (int(x) * 8 for x in rng.integers(-16, 17, 2))
+        share = len(_elements(1 << 20, n, h, tok, head, d)) < n * h * d
+        assert bool(host.self(1 << 20, n, h, tok, head, d)) == share, (n, h, tok, head, d)
+        seen[share] += 1
+    assert min(seen.values()) > 500
+    assert not host.self(1 << 20, 1 << 24, 48, 6144, 128, 128) and host.self(1 << 20, 1 << 24, 49, 6144, 128, 128)
+    assert not host.self(1 << 20, 32767, 32, 128, 32767 * 128, 128)  # [head][token][dim]
+    assert host.self(1 << 20, 1 << 30, 2, 1 << 40, 64, 64)
+
+
 # ------------------------------------------------------------------ calls
 X = PTR * 2
 
@@ -99,3 +118,14 @@ def test_rope_outputs_over_other_tensors(cf, args):
 @pytest.mark.parametrize("qo", [(X + 128, 512, 64), (X - 1024, 512, 64), (X + 16, 512, 64)])
 def test_rope_write8_output_beside_its_input(cf, qo):
     assert _call_both(cf, C.byref(_rope(cf)), C.byref(_cache(cf)), q=(X, 512, 64), qo=qo) == EINVAL
+
+
+@pytest.mark.parametrize("strides", [(128, 64), (64, 128), (192, 128), (0, 64), (512, 0), (512, 32), (64, 64), (-128, 64),
+                                     (32, 512), (384, 192)])
+def test_rows_of_an_output_over_one_another(cf, strides):
+    """Four tokens of four heads of 64, in place and not."""
+    r, c = C.byref(_rope(cf)), C.byref(_cache(cf))
+    for x in (dict(q=(X, *strides), qo=(X, *strides)), dict(q=(PTR * 8, 512, 64), qo=(X, *strides))):
+        assert _call_rope(cf, r, **x, k=(PTR * 4, 512, 64), ko=(PTR * 5, 512, 64)) == EINVAL
+        assert _call_both(cf, r, c, **x) == EINVAL
+    assert _call_rope(cf, r, kv=4, k=(X, 512, 64), ko=(PTR * 5, *strides)) == EINVAL
