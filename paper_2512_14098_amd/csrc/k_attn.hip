@@ -39,10 +39,11 @@ __device__ __forceinline__ void block_reduce(float (&x)[NS + NM], float (*lds)[8
 // How the contexts of one kernel's requests are split.  n workgroups run at a time per
 // key/value head; the candidates are no split, and one and two parts for each of them.  A
 // candidate's time is estimated in keys: its parts in full rounds, or their sum over the
-// workgroups and half a part of tail, whichever is less, and `cost` keys for starting a
-// part and joining its result.
+// workgroups and half a part of tail, whichever is less, and `start` keys for starting a
+// part.  Where some context is split, `join` keys for joining at all and `part` for storing and reading
+// the result of each part.
 struct Split {
-  int n, cost, max_parts;
+  int n, start, part, join, max_parts;
 };
 
 constexpr int kClasses = 18;  // of requests, by the length of their parts
@@ -123,7 +124,8 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
 #pragma unroll
     for (int c = 0; c < 3; c++) {
       const float most = fminf((float)len[k][c], w[2 + k]), per = n[3 * k + c] / (float)sp.n;
-      const float t = fminf(ceilf(per) * most, fmaxf(w[k] / (float)sp.n, most) + 0.5f * most) + per * (float)sp.cost;
+      const float over = n[3 * k + c] > n[3 * k] ? per * (float)sp.part + (float)sp.join : 0.f;
+      const float t = fminf(ceilf(per) * most, fmaxf(w[k] / (float)sp.n, most) + 0.5f * most) + per * (float)sp.start + over;
       if (c == 0 || t < best) {
         best = t;
         part[k] = len[k][c];
@@ -546,11 +548,19 @@ static int desc_groups(const cf_attn_desc *d) {
 }
 
 // Workgroups of the kernels that run at a time per key/value head, as the plan counts on
-// them, and what a part costs beside its keys (measured: starting and joining one takes the
-// few-row kernel as long as 64 keys, the many-row kernel as long as 400; 150 there makes no difference).
+// them, and what a part costs beside its keys.  The few-row kernel takes as long as for 64 keys to start and join
+// one.  Many rows are joined by a kernel that follows, and the parts' results go past the caches: fitted to 832 forms
+// (1 to 16 requests, 20 to 2,100 new tokens on 0 to 59,200, heads of 64 to 256), each whole and with either length of
+// part: 300 keys to join at all and, for each part, 1000 with one wave group, 700 and 250 with two, 100 and
+// 300 above 128 columns, where a key takes three times as long.  With 400 a part, split or not, and nothing for the join,
+// short contexts were split at a loss (32 heads on 8 of 128: a prompt of 200 tokens 22.7 us, 13.3 whole; 20 tokens on 150
+// 17.4 and 12.3), and long ones too (a prompt of 1000, 96 columns: 49 and 27).
 static Split split_of(const cf_attn_desc *d, int kind) {
   const int per_cu = kind ? (desc_groups(d) > 1 || d->head_dim > 128 ? 1 : 2) : (d->head_dim > 128 ? 1 : 2);
-  return Split{(256 * per_cu + d->n_kv_heads - 1) / d->n_kv_heads, kind ? 400 : 64, max_parts(kind)};
+  const int n = (256 * per_cu + d->n_kv_heads - 1) / d->n_kv_heads;
+  if (!kind) return Split{n, 64, 0, 0, max_parts(0)};
+  if (d->head_dim > 128) return Split{n, 0, 300, 100, max_parts(1)};
+  return desc_groups(d) > 1 ? Split{n, 0, 250, 700, max_parts(1)} : Split{n, 0, 1000, 300, max_parts(1)};
 }
 
 uint64_t plan_view(const cf_attn_desc *d, PlanView *v) {

@@ -1,0 +1,35 @@
+"""Which contexts of many-row requests a plan splits."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def cf():
+    from paper_2512_14098_amd import cf as _cf
+    return _cf
+
+
+def _split_tiles(cf, lens, new, heads, kv_heads, dim):
+    start = torch.tensor([0] + new, device="cuda").cumsum(0).int()
+    plan = cf.cf_attn_plan(start, torch.tensor(lens, dtype=torch.int32, device="cuda"), sum(new), max(new), heads, kv_heads, dim)
+    return int(plan.work[16:20].view(torch.int32))  # the header's count
+
+
+@pytest.mark.parametrize("lens,new,heads,kv_heads,dim", [
+    ([200], [200], 32, 8, 128), ([170], [20], 32, 8, 128), ([214] * 4, [64] * 4, 32, 8, 128), ([500], [500], 32, 8, 128),
+    ([1500] * 15 + [200], [1] * 15 + [200], 32, 8, 128), ([200], [200], 16, 4, 64), ([900] * 4, [500] * 4, 16, 4, 64),
+    ([1000], [1000], 32, 8, 96), ([600] * 4, [200] * 4, 32, 8, 96), ([200], [200], 16, 8, 256), ([400], [400], 16, 16, 256), ([214] * 4, [64] * 4, 16, 8, 256)])
+def test_whole_where_the_join_costs_more(cf, lens, new, heads, kv_heads, dim):
+    """A join takes about as long as 300 keys (100 above 128 columns), storing and reading the parts more where they
+    fill the card: contexts that gain less stay whole."""
+    assert _split_tiles(cf, lens, new, heads, kv_heads, dim) == 0
+
+
+@pytest.mark.parametrize("lens,new,heads,kv_heads,dim", [
+    ([1040], [40], 32, 8, 128), ([30005] * 3, [5] * 3, 32, 8, 128), ([1220] * 4, [20] * 4, 32, 8, 128),
+    ([10100] * 2, [100] * 2, 32, 8, 128), ([2520], [20], 16, 8, 256), ([8200], [200], 8, 1, 128), ([20500], [500], 16, 2, 64)])
+def test_split_where_one_round_leaves_the_card_empty(cf, lens, new, heads, kv_heads, dim):
+    assert _split_tiles(cf, lens, new, heads, kv_heads, dim) > 0
