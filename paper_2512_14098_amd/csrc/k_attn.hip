@@ -136,6 +136,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
   // the last two are bounded by the choice of the part whatever the lengths are.
   int64_t at[2] = {0, 0};
   int slots[2] = {0, 0}, joins[2] = {0, 0};
+  const bool order = 2.f * n[0] >= (float)sp0.n;
   for (int c0 = 0; c0 < n_seq; c0 += NT) {
     const int i = c0 + tid, cn = min(NT, n_seq - c0);
     int tiles = c0 ? 0 : tiles0, kind = c0 ? 0 : kind0, keys = c0 ? 0 : keys0;
@@ -146,36 +147,41 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
     const int parts = max((int)((unsigned)(keys + (unsigned)part[kind] - 1u) / (unsigned)part[kind]), 1);
     // Long parts first, so that the last workgroups to start are short: a stable sort by the length of a
     // part in 16 classes (256 decodes of 300 to 4300 keys: 282 us, 292 with three classes; 8-bit cache
-    // 162 and 169).  Not for the many-row kernel, whose neighbouring tiles of one request share keys
-    // in the L2: its requests come last, in order, and after them those without tiles.
+    // 162 and 169; in order of the requests 64 decodes 70 us, 66 sorted, 256 268 and 233).  Not for the many-row kernel, whose
+    // neighbouring tiles of one request share keys in the L2: its requests come last, in order, and after them those
+    // without tiles.  Nor for fewer tiles than half of the workgroups that run at a time (32 decodes 49 us either
+    // way): all start at once, and the sort takes 0.9 of the plan's 6.9 us.
     const int lane = tid & 63, wv = tid >> 6;
-    const float most = fminf((float)part[0], w[2]), mine_len = fminf((float)keys, (float)part[0]);
-    const int cls = tiles == 0 ? kClasses - 1 : kind ? kClasses - 2 : 15 - (int)(mine_len / fmaxf(most, 1.f) * 15.99f);
-    int rank = 0, n_cls = 0;  // among the wave's of the class; lane c: how many of class c
-#pragma unroll
-    for (int c = 0; c < kClasses; c++) {
-      const uint64_t same = __ballot(cls == c);
-      if (cls == c) rank = __builtin_popcountll(same & ((1ull << lane) - 1));
-      if (lane == c) n_cls = __builtin_popcountll(same);
-    }
+    int rank = tid;
     __syncthreads();  // the items of the requests before have been written
-    if (lane < kClasses) l_cls[wv][lane] = n_cls;
-    __syncthreads();
-    int first = 0, all = 0;
-    if (lane < kClasses)
+    if (order) {
+      const float most = fminf((float)part[0], w[2]), mine_len = fminf((float)keys, (float)part[0]);
+      const int cls = tiles == 0 ? kClasses - 1 : kind ? kClasses - 2 : 15 - (int)(mine_len / fmaxf(most, 1.f) * 15.99f);
+      int n_cls = 0;  // rank among the wave's of the class; lane c: how many of class c
 #pragma unroll
-      for (int e = 0; e < NT / 64; e++) {
-        const int y = l_cls[e][lane];
-        if (e < wv) first += y;
-        all += y;
+      for (int c = 0; c < kClasses; c++) {
+        const uint64_t same = __ballot(cls == c);
+        if (cls == c) rank = __builtin_popcountll(same & ((1ull << lane) - 1));
+        if (lane == c) n_cls = __builtin_popcountll(same);
       }
-    int incl_cls = all;
+      if (lane < kClasses) l_cls[wv][lane] = n_cls;
+      __syncthreads();
+      int first = 0, all = 0;
+      if (lane < kClasses)
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up(incl_cls, o);
-      if (lane >= o) incl_cls += y;
+        for (int e = 0; e < NT / 64; e++) {
+          const int y = l_cls[e][lane];
+          if (e < wv) first += y;
+          all += y;
+        }
+      int incl_cls = all;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up(incl_cls, o);
+        if (lane >= o) incl_cls += y;
+      }
+      rank += __shfl(first + incl_cls - all, cls);
     }
-    rank += __shfl(first + incl_cls - all, cls);
     l_rows[rank][0] = q0;
     l_rows[rank][1] = nq;
     l_rows[rank][2] = nk;
