@@ -43,7 +43,8 @@ struct Int {
   static constexpr int value = N;
 };
 
-// Two of the four e4m3 codes of a word, times a power of two, as a pair of elements.
+// Two of the four e4m3 codes of a word, times a power of two, as a pair of elements.  The conversion reads the
+// scale's exponent field alone: bits of 0 are 2^-127, not 0, and those of infinity NaN.
 template <typename T>
 __device__ __forceinline__ uint32_t widen8(uint32_t codes, float scale, int half) {
   if constexpr (__is_same(T, __bf16))
