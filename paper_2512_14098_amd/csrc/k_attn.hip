@@ -41,7 +41,7 @@ __device__ __forceinline__ void block_reduce(float (&x)[NS + NM], float (*lds)[8
 // candidate's time is estimated in keys: its parts in full rounds, or their sum over the
 // workgroups and half a part of tail, whichever is less, and `start` keys for starting a
 // part.  Where some context is split, `join` keys for joining at all and `part` for storing and reading
-// the result of each part.
+// the result of each part, less where tiles are not full: only rows that there are have one.
 struct Split {
   int n, start, part, join, max_parts;
 };
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
       len[k][c] = (max((int)even, least) + 127) & ~127;
     }
   }
-  float n[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  float n[7] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // parts of either kernel's candidates; rows of the many-row kernel
   for (int i = tid; i < n_seq; i += NT) {
     int tiles = tiles0, kind = kind0, keys = keys0;
     if (i != tid) load(i, tiles, kind, keys);
@@ -113,8 +113,17 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
       n[c] += kind ? 0.f : t;
       n[3 + c] += kind ? t : 0.f;
     }
+    n[6] += kind ? (float)(i == tid ? first_nq : nq) * (float)G : 0.f;
   }
-  block_reduce<NT, 6, 0>(n, red);
+  if (few_only) {  // a decode step's: the other sums are zero
+    float few[3] = {n[0], n[1], n[2]};
+    block_reduce<NT, 3, 0>(few, red);
+#pragma unroll
+    for (int c = 0; c < 3; c++) n[c] = few[c];
+  } else {
+    block_reduce<NT, 7, 0>(n, red);
+  }
+  const float full = n[6] / fmaxf(n[3] * (float)(1 << big_log2), 1.f);  // of the rows of the many-row kernel's tiles
   int part[2];
 #pragma unroll
   for (int k = 0; k < 2; k++) {
@@ -124,7 +133,7 @@ __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_s
 #pragma unroll
     for (int c = 0; c < 3; c++) {
       const float most = fminf((float)len[k][c], w[2 + k]), per = n[3 * k + c] / (float)sp.n;
-      const float over = n[3 * k + c] > n[3 * k] ? per * (float)sp.part + (float)sp.join : 0.f;
+      const float over = n[3 * k + c] > n[3 * k] ? per * (float)sp.part * full + (float)sp.join : 0.f;
       const float t = fminf(ceilf(per) * most, fmaxf(w[k] / (float)sp.n, most) + 0.5f * most) + per * (float)sp.start + over;
       if (c == 0 || t < best) {
         best = t;
@@ -555,18 +564,19 @@ static int desc_groups(const cf_attn_desc *d) {
 
 // Workgroups of the kernels that run at a time per key/value head, as the plan counts on
 // them, and what a part costs beside its keys.  The few-row kernel takes as long as for 64 keys to start and join
-// one.  Many rows are joined by a kernel that follows, and the parts' results go past the caches: fitted to 832 forms
-// (1 to 16 requests, 20 to 2,100 new tokens on 0 to 59,200, heads of 64 to 256), each whole and with either length of
-// part: 300 keys to join at all and, for each part, 1000 with one wave group, 700 and 250 with two, 100 and
-// 300 above 128 columns, where a key takes three times as long.  With 400 a part, split or not, and nothing for the join,
+// one.  Many rows are joined by a kernel that follows, and the parts' results go past the caches: fitted to 1,140 forms
+// (1 to 40 requests, 1 to 2,100 new tokens on 0 to 59,200, heads of 64 to 256), each whole and with either length of
+// part: 250 keys to join at all and, for each part of full tiles, 1500 with one wave group, 700 and 250 with two, 50 and
+// 600 above 128 columns, where a key takes three times as long.  With 400 a part, split or not, and nothing for the join,
 // short contexts were split at a loss (32 heads on 8 of 128: a prompt of 200 tokens 22.7 us, 13.3 whole; 20 tokens on 150
-// 17.4 and 12.3), and long ones too (a prompt of 1000, 96 columns: 49 and 27).
+// 17.4 and 12.3), and long ones too (a prompt of 1000, 96 columns: 49 and 27).  With each part's cost that of a full tile, 5 tokens on each
+// of three contexts of 30,000, 20 of a tile's 128 rows, had 22 parts each, not 40: 111 us and 89.
 static Split split_of(const cf_attn_desc *d, int kind) {
   const int per_cu = kind ? (desc_groups(d) > 1 || d->head_dim > 128 ? 1 : 2) : (d->head_dim > 128 ? 1 : 2);
   const int n = (256 * per_cu + d->n_kv_heads - 1) / d->n_kv_heads;
   if (!kind) return Split{n, 64, 0, 0, max_parts(0)};
-  if (d->head_dim > 128) return Split{n, 0, 300, 100, max_parts(1)};
-  return desc_groups(d) > 1 ? Split{n, 0, 250, 700, max_parts(1)} : Split{n, 0, 1000, 300, max_parts(1)};
+  if (d->head_dim > 128) return Split{n, 0, 600, 50, max_parts(1)};
+  return desc_groups(d) > 1 ? Split{n, 0, 250, 700, max_parts(1)} : Split{n, 0, 1500, 250, max_parts(1)};
 }
 
 uint64_t plan_view(const cf_attn_desc *d, PlanView *v) {

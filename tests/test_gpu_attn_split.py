@@ -23,7 +23,7 @@ def _split_tiles(cf, lens, new, heads, kv_heads, dim):
     ([1500] * 15 + [200], [1] * 15 + [200], 32, 8, 128), ([200], [200], 16, 4, 64), ([900] * 4, [500] * 4, 16, 4, 64),
     ([1000], [1000], 32, 8, 96), ([600] * 4, [200] * 4, 32, 8, 96), ([200], [200], 16, 8, 256), ([400], [400], 16, 16, 256), ([214] * 4, [64] * 4, 16, 8, 256)])
 def test_whole_where_the_join_costs_more(cf, lens, new, heads, kv_heads, dim):
-    """A join takes about as long as 300 keys (100 above 128 columns), storing and reading the parts more where they
+    """A join takes about as long as 250 keys (50 above 128 columns), storing and reading the parts more where they
     fill the card: contexts that gain less stay whole."""
     assert _split_tiles(cf, lens, new, heads, kv_heads, dim) == 0
 
@@ -33,3 +33,11 @@ def test_whole_where_the_join_costs_more(cf, lens, new, heads, kv_heads, dim):
     ([10100] * 2, [100] * 2, 32, 8, 128), ([2520], [20], 16, 8, 256), ([8200], [200], 8, 1, 128), ([20500], [500], 16, 2, 64)])
 def test_split_where_one_round_leaves_the_card_empty(cf, lens, new, heads, kv_heads, dim):
     assert _split_tiles(cf, lens, new, heads, kv_heads, dim) > 0
+
+
+def test_parts_of_tiles_with_few_rows(cf):
+    """Their results cost little: two parts for each workgroup that runs at a time (64 for each of 8 heads), not one:
+    90,015 keys in parts of an even share of 704, up to a multiple of 128."""
+    start = torch.tensor([0, 5, 10, 15], dtype=torch.int32, device="cuda")
+    plan = cf.cf_attn_plan(start, torch.full((3,), 30005, dtype=torch.int32, device="cuda"), 15, 5, 32, 8, 128)
+    assert int(plan.work[4:8].view(torch.int32)) == 3 * -(-30005 // 768)  # the header's count of the many-row kernel's items

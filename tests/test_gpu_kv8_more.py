@@ -116,7 +116,7 @@ def test_long_reads(cf, kind, heads, dim, page):
 
 # ------------------------------------------------------------------ joins
 @pytest.mark.parametrize("width", [16, 8])
-@pytest.mark.parametrize("kind,heads,kv_heads,dim,new,lens", [("bf16", 8, 1, 64, 8320, 12000), ("fp16", 16, 2, 48, 4170, 12001)])
+@pytest.mark.parametrize("kind,heads,kv_heads,dim,new,lens", [("bf16", 8, 1, 64, 8320, 40000), ("fp16", 16, 2, 48, 4170, 40001)])
 def test_joined_tiles_outnumber_the_joining_workgroups(cf, width, kind, heads, kv_heads, dim, new, lens):
     """A few more tiles than run at a time, all of them split: 520 and 2 x 261.  Only heads of 64 columns or fewer
     have so many: a plan splits fewer tiles than twice the workgroups that run at a time, 512 or, of other widths with so
