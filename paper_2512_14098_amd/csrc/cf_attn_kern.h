@@ -212,8 +212,9 @@ __device__ __forceinline__ bool read_item(const AttnArgs &a, int kind, int item,
   return true;
 }
 
-// The parts of a split context are joined in part order:  m = max m_p, l = sum l_p e^(m_p - m),
-// o = sum o_p e^(m_p - m) / l.
+// The parts of a split context are joined:  m = max m_p, l = sum l_p e^(m_p - m), o = sum o_p e^(m_p - m) / l, in an
+// order that the sizes alone decide, so that results repeat: with few rows part by part, with many every fourth
+// part by one of four lanes (l) and every share-th by one of `share` threads (o), then those.
 
 // Few rows: by the workgroup that finishes last, whichever it is.
 // w: LDS of this workgroup, at least 2 x max_parts x kRowsSmall floats.
@@ -413,7 +414,7 @@ __device__ __forceinline__ void matrix_order() {
 // patches, 16 heads, 53 us, 0.54 PFLOP/s, matrix unit busy 36 %.  Above 128 columns a
 // wave's state does not fit the registers (32 of them spilled, 55 over a cache): one
 // causal sequence of 4096 tokens, 16 heads of 256, 241 us, 0.57 PFLOP/s; two chunks of
-// 1000 tokens on 24001, 32 heads on 8, 3.4 ms, 0.48 PFLOP/s.  136 to 248 columns take as long.
+// 1000 tokens on 24001, 32 heads on 8, 3.8 ms, 0.42 PFLOP/s.  136 to 248 columns take as long.
 // C8, an 8-bit cache: codes are widened between registers and LDS, half the bytes are loaded and staged.
 // Lanes hold the addresses of 16 keys' codes and exponents; worked out by the scalar unit at each load from a row number
 // they cost a third (two chunks of 1000 on 24001, 32 heads on 8: 925 us against 719; the 16-bit cache 746).

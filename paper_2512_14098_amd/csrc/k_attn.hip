@@ -51,8 +51,8 @@ constexpr int kClasses = 18;  // of requests, by the length of their parts
 // One workgroup.  Pass 1 sums the work of either kernel, (row tiles) x (keys), and the
 // parts that each candidate length gives; pass 2 takes NT requests at a time, places their
 // items by a scan and writes them, a thread per item.  Bound by the latency of its few
-// steps (16 to 256 requests: 7 us; with 64-bit divisions and a scan for each count 17), so that 256 threads do better than 1024 as long as
-// one step takes all requests.
+// steps (4 to 16 requests 6 us, 64 7 us, 256 8 to 10; with 64-bit divisions and a scan for each count 17), so that 256
+// threads do better than 1024 as long as one step takes all requests.
 template <int NT>
 __global__ __launch_bounds__(NT) void k_attn_plan(PlanView v, const int32_t *q_start, const int32_t *kv_len, int n_seq,
                                                   int n_tok, int G, int Hkv, int few_only, int big_log2, Split sp0,
