@@ -651,7 +651,7 @@ cf_status cf_attn_prompt(const cf_attn_seqs *a, float scale, void *out_dev, floa
  * Cache: one layer's keys and values, e4m3 codes [n_pages][n_kv_heads][page][head_dim] each, and
  * a byte per row of either, [n_pages][n_kv_heads][2][page], keys' before values': the row's scale is
  * 2^(byte - 127), byte 255 makes it NaN.  Pages and slots as above; head_dim is a multiple of 16, 16..256; pointers
- * are 16-byte aligned.  A row x is written with the smallest scale 2^e, e >= -126, such that
+ * are 16-byte aligned; arrays of a cache that is written do not overlap.  A row x is written with the smallest scale 2^e, e >= -126, such that
  * max |x| <= 448 * 2^e over its finite elements, and each element as the nearest code to x * 2^-e,
  * ties to even; |x| is cut at 61440 in fp16 and 1.875 * 2^127 in bf16, so that every value held is one of the
  * element type; reading rounds to the dtype asked for (a cache written in bf16 and read in fp16
@@ -684,7 +684,7 @@ cf_status cf_rope(const cf_rope_desc *r, int32_t n_tok, int32_t n_heads, int32_t
 
 /* cf_kv_write into the 8-bit cache.  Slots outside the cache are skipped.  The slots of a call's
  * tokens differ: one that is given twice holds codes and a scale of either token.
- * Errors: CF_EINVAL (sizes, alignment, NULL arrays). */
+ * Errors: CF_EINVAL (sizes, alignment, NULL arrays, arrays of the cache that overlap). */
 cf_status cf_kv_write8(const cf_kv_cache8 *cache, int32_t n_tok, const void *k_dev, int64_t k_tok, int64_t k_head,
                        const void *v_dev, int64_t v_tok, int64_t v_head, const int64_t *slot_dev, void *stream);
 
@@ -709,7 +709,7 @@ cf_status cf_attn_paged8(const cf_attn_desc *d, const cf_kv_cache8 *cache, const
  * k_start_dev[i+1] - k_start_dev[i] - 1, found by its row of table_dev [n_seq][max_pages], are rows k_start_dev[i] .. of
  * k_out_dev and v_out_dev [n_tok][n_kv_heads][head_dim], as cf_attn_prompt takes them.  Pages outside the cache
  * and positions past the table's row read as zeros; rows of no request are left as they were.
- * Errors: CF_EINVAL (sizes, alignment, NULL arrays). */
+ * Errors: CF_EINVAL (sizes, alignment, NULL arrays, outputs that overlap). */
 cf_status cf_kv_read8(const cf_kv_cache8 *cache, const int32_t *table_dev, int32_t max_pages, int32_t n_seq,
                       const int32_t *k_start_dev, int32_t n_tok, void *k_out_dev, void *v_out_dev, void *stream);
 

@@ -10,6 +10,12 @@ struct RowSet {
   int64_t n, heads, tok, head, d;
 };
 
+// Whether two ranges of bytes meet.
+inline bool bytes_meet(const void *p, uint64_t np, const void *q, uint64_t nq) {
+  const uint64_t a = (uint64_t)(uintptr_t)p, b = (uint64_t)(uintptr_t)q;
+  return np > 0 && nq > 0 && (a <= b ? b - a < np : a - b < nq);
+}
+
 namespace overlap {
 
 constexpr int64_t kFar = 1ll << 56;  // elements: no memory reaches that far

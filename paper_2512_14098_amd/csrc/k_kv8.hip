@@ -410,6 +410,10 @@ cf_status take_write(const cf_kv_cache8 *c, const void *k, int64_t k_tok, int64_
   if (!k || !v || !slot) return set_error(CF_EINVAL, "NULL array");
   if (!rows_ok(k, k_tok, k_head) || !rows_ok(v, v_tok, v_head))
     return set_error(CF_EINVAL, "keys and values are not 16-byte aligned");
+  const uint64_t rows = (uint64_t)c->n_pages * c->n_kv_heads * c->page, codes = rows * c->head_dim;
+  if (bytes_meet(c->k_dev, codes, c->v_dev, codes) || bytes_meet(c->exp_dev, 2 * rows, c->k_dev, codes) ||
+      bytes_meet(c->exp_dev, 2 * rows, c->v_dev, codes))
+    return set_error(CF_EINVAL, "arrays of a cache that is written overlap");
   a->k = k; a->k_tok = k_tok; a->k_head = k_head;
   a->v = v; a->v_tok = v_tok; a->v_head = v_head;
   a->kc = (uint8_t *)c->k_dev; a->vc = (uint8_t *)c->v_dev; a->ec = c->exp_dev;
@@ -537,6 +541,8 @@ extern "C" cf_status cf_kv_read8(const cf_kv_cache8 *cache, const int32_t *table
   if (n_tok == 0) return CF_OK;
   if (!table_dev || !k_start_dev || !k_out_dev || !v_out_dev) return set_error(CF_EINVAL, "NULL array");
   if (((uintptr_t)k_out_dev | (uintptr_t)v_out_dev) & 15) return set_error(CF_EINVAL, "output is not 16-byte aligned");
+  const uint64_t out_bytes = 2ull * n_tok * cache->n_kv_heads * cache->head_dim;
+  if (bytes_meet(k_out_dev, out_bytes, v_out_dev, out_bytes)) return set_error(CF_EINVAL, "outputs overlap");
   ReadArgs a;
   a.kc = (const uint8_t *)cache->k_dev; a.vc = (const uint8_t *)cache->v_dev; a.ec = cache->exp_dev;
   a.table = table_dev; a.start = k_start_dev;

@@ -101,3 +101,22 @@ def test_rope_in_place_refuses_rows_over_one_another(cf):
         q = base.as_strided(size, strides)
         want = cf.cf_rope(q, None, *t)
         assert cf.cf_rope(q, None, *t, in_place=True) is q and torch.equal(q, want)
+
+
+def test_writes_refuse_one_array_for_keys_and_values(cf):
+    """Reads and attention take keys for values."""
+    rng = np.random.default_rng(3)
+    k, v, e = _cache(4, 2, 16, 64)
+    x = _rand(5, (8, 4, 64), "bf16")
+    slots = torch.arange(8).cuda()
+    before = _cells(k, v, e)
+    with pytest.raises(cf.CfError, match="overlap"):
+        cf.cf_kv_write8(x[:, :2], x[:, 2:], k, k, e, slots)
+    with pytest.raises(cf.CfError, match="overlap"):
+        cf.cf_rope_write8(x, x[:, :2], x[:, 2:], *_dev(*_turning(rng, 8, 64, 1)), k, k, e, slots)
+    for a, b in zip(before, _cells(k, v, e)):
+        assert np.array_equal(a, b)
+    table, start = torch.arange(4, dtype=torch.int32).cuda()[None], torch.tensor([0, 50], dtype=torch.int32).cuda()
+    kk, _ = cf.cf_kv_read8(k, k, e, table, start, 50)
+    want, _ = cf.cf_kv_read8(k, v, e, table, start, 50)
+    assert torch.equal(kk, want)

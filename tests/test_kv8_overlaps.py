@@ -6,7 +6,8 @@ import subprocess
 import numpy as np
 import pytest
 
-from tests.test_kv8_refusals import EINVAL, PTR, ROOT, _cache, _call_both, _call_rope, _rope, cf, pytestmark  # noqa: F401
+from tests.test_kv8_refusals import (EINVAL, OK, PTR, ROOT, _cache, _call_both, _call_read, _call_rope, _call_write,  # noqa: F401
+                                     _rope, cf, pytestmark)
 
 CSRC = os.path.join(ROOT, "paper_2512_14098_amd", "csrc")
 
@@ -24,10 +25,11 @@ extern "C" int meet(int64_t a, int64_t b, int64_t n, int64_t ha, int64_t hb, int
 extern "C" int self(int64_t a, int64_t n, int64_t h, int64_t t, int64_t s, int64_t d) {
   return cf::rows_overlap(cf::RowSet{(void *)a, n, h, t, s, d});
 }
+extern "C" int bytes(int64_t p, int64_t np, int64_t q, int64_t nq) { return cf::bytes_meet((void *)p, np, (void *)q, nq); }
 """)
     subprocess.check_call(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", CSRC, str(d / "o.cpp"), "-o", str(d / "o.so")])
     lib = C.CDLL(str(d / "o.so"))
-    lib.meet.argtypes, lib.self.argtypes = [C.c_int64] * 10, [C.c_int64] * 6
+    lib.meet.argtypes, lib.self.argtypes, lib.bytes.argtypes = [C.c_int64] * 10, [C.c_int64] * 6, [C.c_int64] * 4
     return lib
 
 
@@ -85,8 +87,27 @@ def test_rows_overlap(host):
     assert host.self(1 << 20, 1 << 30, 2, 1 << 40, 64, 64)
 
 
+def test_bytes_meet(host):
+    for p, np_, q, nq in np.random.default_rng(2).integers(0, 12, (2000, 4)):
+        p, np_, q, nq = (int(x) for x in (p, np_, q, nq))
+        assert bool(host.bytes(p, np_, q, nq)) == bool(set(range(p, p + np_)) & set(range(q, q + nq)))
+    assert not host.bytes(1 << 62, 1 << 62, 1 << 61, 1 << 61) and host.bytes(1 << 62, 1 << 62, 1 << 61, (1 << 61) + 1)
+
+
 # ------------------------------------------------------------------ calls
 X = PTR * 2
+# 10 pages of 2 heads of 16 rows of 64: 20,480 bytes of codes each, 640 of exponents
+APART = dict(k_dev=PTR, v_dev=PTR + 20480, exp_dev=PTR + 40960)
+
+
+def _apart(cf, **kw):
+    return C.byref(_cache(cf, **dict(APART, **kw)))
+
+
+def _last(cf):
+    buf = C.create_string_buffer(256)
+    cf.lib().cf_last_error(buf, 256)
+    return buf.value
 
 
 @pytest.mark.parametrize("args", [
@@ -96,9 +117,9 @@ X = PTR * 2
     dict(q=(X, 512, 64), qo=(X, 512, 64), v=(X + 7 * 128, 512, 64)),  # the second value head is the next token's query
     dict(qo=(X, 256, 64), k=(X + 512, 0, 64)),  # keys of one token for all, inside the output
     dict(qo=(X, 256, 64), v=(X + 1024, 512, 64)),  # another token stride
-    dict(qo=(PTR + 16, 256, 64))])
+    dict(q=(X, 512, 64), qo=(PTR + 16, 256, 64))])
 def test_rope_write8_output_over_keys_or_values(cf, args):
-    assert _call_both(cf, C.byref(_rope(cf)), C.byref(_cache(cf)), **args) == EINVAL
+    assert _call_both(cf, C.byref(_rope(cf)), _apart(cf), **args) == EINVAL and b"k_dev or v_dev" in _last(cf)
 
 
 @pytest.mark.parametrize("args", [
@@ -112,20 +133,61 @@ def test_rope_write8_output_over_keys_or_values(cf, args):
     dict(q=(X, 512, 64), qo=(X - 1024, 512, 64)),
     dict(k=(X, 512, 64), ko=(X + 64, 512, 64), qo=(PTR * 5, 256, 64))])
 def test_rope_outputs_over_other_tensors(cf, args):
-    assert _call_rope(cf, C.byref(_rope(cf)), **args) == EINVAL
+    assert _call_rope(cf, C.byref(_rope(cf)), **args) == EINVAL and b"shares elements" in _last(cf)
 
 
 @pytest.mark.parametrize("qo", [(X + 128, 512, 64), (X - 1024, 512, 64), (X + 16, 512, 64)])
 def test_rope_write8_output_beside_its_input(cf, qo):
-    assert _call_both(cf, C.byref(_rope(cf)), C.byref(_cache(cf)), q=(X, 512, 64), qo=qo) == EINVAL
+    assert _call_both(cf, C.byref(_rope(cf)), _apart(cf), q=(X, 512, 64), qo=qo) == EINVAL and b"with its input" in _last(cf)
 
 
 @pytest.mark.parametrize("strides", [(128, 64), (64, 128), (192, 128), (0, 64), (512, 0), (512, 32), (64, 64), (-128, 64),
                                      (32, 512), (384, 192)])
 def test_rows_of_an_output_over_one_another(cf, strides):
     """Four tokens of four heads of 64, in place and not."""
-    r, c = C.byref(_rope(cf)), C.byref(_cache(cf))
+    r, c = C.byref(_rope(cf)), _apart(cf)
     for x in (dict(q=(X, *strides), qo=(X, *strides)), dict(q=(PTR * 8, 512, 64), qo=(X, *strides))):
-        assert _call_rope(cf, r, **x, k=(PTR * 4, 512, 64), ko=(PTR * 5, 512, 64)) == EINVAL
-        assert _call_both(cf, r, c, **x) == EINVAL
-    assert _call_rope(cf, r, kv=4, k=(X, 512, 64), ko=(PTR * 5, *strides)) == EINVAL
+        assert _call_rope(cf, r, **x, k=(PTR * 4, 512, 64), ko=(PTR * 5, 512, 64)) == EINVAL and b"rows" in _last(cf)
+        assert _call_both(cf, r, c, **x) == EINVAL and b"rows" in _last(cf)
+    assert _call_rope(cf, r, kv=4, k=(X, 512, 64), ko=(PTR * 5, *strides)) == EINVAL and b"rows" in _last(cf)
+
+
+# ------------------------------------------------------------------ arrays of the cache, outputs of a read
+@pytest.mark.parametrize("over", [dict(v_dev=PTR), dict(v_dev=PTR + 20480 - 16), dict(k_dev=PTR + 40960 - 32),
+                                  dict(exp_dev=PTR + 20480 - 16), dict(exp_dev=PTR + 40960 - 16), dict(exp_dev=PTR - 624)])
+def test_arrays_of_a_cache_over_one_another(cf, over):
+    """Writes are refused; reads and attention may take keys for values too."""
+    c = _apart(cf, **over)
+    assert _call_write(cf, c) == EINVAL and b"overlap" in _last(cf)
+    assert _call_both(cf, C.byref(_rope(cf)), c, q=(X, 512, 64), qo=(X, 512, 64)) == EINVAL and b"overlap" in _last(cf)
+    assert _call_write(cf, c, n=0) == OK
+
+
+def test_outputs_of_a_read_over_one_another(cf):
+    for k, v in ((PTR, PTR), (PTR, PTR + 1280 - 16), (PTR + 1280 - 16, PTR)):  # 5 tokens of 2 heads of 64
+        assert _call_read(cf, _apart(cf), k=k, v=v) == EINVAL and b"overlap" in _last(cf)
+
+
+@pytest.mark.parametrize("bad,says", [
+    (dict(n=-1), b"n_tok"), (dict(k=(None, 512, 64)), b"NULL"), (dict(v=(None, 512, 64)), b"NULL"), (dict(slots=None), b"NULL"),
+    (dict(k=(PTR + 8, 512, 64)), b"aligned"), (dict(v=(PTR, 512, 60)), b"aligned"), (dict(k=(PTR, 4, 64)), b"aligned")])
+def test_writes_into_arrays_apart(cf, bad, says):
+    """What a write refuses, each for its own reason."""
+    assert _call_write(cf, _apart(cf), **bad) == EINVAL and says in _last(cf)
+    assert _call_both(cf, C.byref(_rope(cf)), _apart(cf), **bad) == EINVAL and says in _last(cf)
+
+
+@pytest.mark.parametrize("bad,says", [
+    (dict(heads=0), b"n_heads"), (dict(heads=65536), b"n_heads"), (dict(q=(None, 512, 64)), b"NULL"),
+    (dict(qo=(None, 512, 64)), b"NULL"), (dict(q=(PTR + 4, 512, 64)), b"aligned"), (dict(qo=(PTR, 512, 65)), b"aligned"),
+    (dict(qo=(PTR, 256, 64)), b"in place")])
+def test_turned_writes_into_arrays_apart(cf, bad, says):
+    assert _call_both(cf, C.byref(_rope(cf)), _apart(cf), **bad) == EINVAL and says in _last(cf)
+
+
+@pytest.mark.parametrize("bad,says", [
+    (dict(table=None), b"NULL"), (dict(most=0), b"max_pages"), (dict(n_seq=0), b"n_seq"), (dict(n_seq=(1 << 30) + 1), b"n_seq"),
+    (dict(start=None), b"NULL"), (dict(n_tok=-1), b"n_tok"), (dict(k=None), b"NULL"), (dict(v=None), b"NULL"),
+    (dict(k=PTR + 8), b"aligned"), (dict(v=PTR + 4), b"aligned")])
+def test_reads_into_outputs_apart(cf, bad, says):
+    assert _call_read(cf, _apart(cf), **dict(dict(v=PTR * 2), **bad)) == EINVAL and says in _last(cf)
