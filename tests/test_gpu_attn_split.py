@@ -1,5 +1,9 @@
 """Which contexts of many-row requests a plan splits."""
+import numpy as np
 import pytest
+
+from tests.test_gpu_attn import _compare, _say
+from tests.test_gpu_attn_join import Caches
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +45,19 @@ def test_parts_of_tiles_with_few_rows(cf):
     start = torch.tensor([0, 5, 10, 15], dtype=torch.int32, device="cuda")
     plan = cf.cf_attn_plan(start, torch.full((3,), 30005, dtype=torch.int32, device="cuda"), 15, 5, 32, 8, 128)
     assert int(plan.work[4:8].view(torch.int32)) == 3 * -(-30005 // 768)  # the header's count of the many-row kernel's items
+
+
+@pytest.mark.parametrize("width", [16, 8])
+@pytest.mark.parametrize("n,busy,many", [(250, 20, 3), (255, 3, 40), (2600, 30, 5), (2600, 700, 9)])
+def test_plans_in_order_and_sorted(cf, width, n, busy, many):
+    """Requests that wait, with one new token and with many in any order, in one and in three rounds of the plan's
+    workgroup; 700 with few rows are sorted by length, fewer are not."""
+    _say("order", width, n, busy, many)
+    rng = np.random.default_rng(n + busy)
+    new = np.zeros(n, int)
+    at = rng.permutation(n)
+    new[at[:busy]] = rng.integers(1, 5, busy)
+    new[at[busy:busy + many]] = rng.integers(10, 60, many)
+    lens = np.maximum(new, np.where(new > 0, rng.integers(1, 300, n), rng.integers(1, 20, n)))
+    c = Caches(cf, "bf16", lens.tolist(), new.tolist(), 4, 1, 64)
+    _compare(*c.run(width, c.plan()), c.want("bf16"))
